@@ -73,7 +73,9 @@ typedef enum {
   EF_ERR_INVALID_MASK = 10,        /* local attention: window < 1 or sinks < 0 */
   EF_ERR_INVALID_DIFF = 11,        /* differential attention: lambda_init or eps not finite, or eps < 0 */
   EF_ERR_INVALID_SPLIT = 12,       /* d_splits not 1, 2 or 4, or more than 8 query rows per kv head */
-  EF_ERR_SCRATCH_TOO_SMALL = 13    /* the problem needs more than EF_STATIC_SCRATCH_BYTES of scratch */
+  EF_ERR_SCRATCH_TOO_SMALL = 13,   /* the problem needs more than EF_STATIC_SCRATCH_BYTES of scratch */
+  EF_ERR_INVALID_BLOCKS = 14       /* block_size not 64 or 128, more than EF_MAX_BLOCKS blocks, or topk,
+                                      sink_blocks, local_blocks or new_keys out of range */
 } ef_status;
 
 /* Version of this ABI (EF_ABI_VERSION). */
@@ -410,6 +412,68 @@ ef_status ef_attention_splitkv_noalloc(const void* q, const void* k, const void*
                                        int B, int Hq, int Hkv, int Sq, int Skv, int D,
                                        float scale, int causal, int partition_size,
                                        void* stream);
+
+/*
+ * Long contexts: block-sparse attention and shared prefixes
+ *
+ * The entry points below serve long contexts: attention over selected blocks of
+ * the key axis (the blocks' summaries, the choice of each query's blocks, the
+ * attention over them) and attention of a batch of sequences over one prefix.
+ * They follow the conventions at the top of this file, and in addition:
+ *   - lengths : device buffer of B int32, or NULL. Sequence b has
+ *     len_b = lengths[b] valid keys (clamped to [0, Skv]); Skv, the extent of its
+ *     buffers, is then a capacity. With NULL every sequence has Skv keys. What lies
+ *     behind a sequence's length is never read. Keys and values below it must be
+ *     finite.
+ *   - Query i of sequence b sits at key n_i = i + len_b - Sq of its sequence (its
+ *     queries are its last Sq positions); a negative n_i sees nothing.
+ *   - o is bf16, the type the next product takes: one rounding of an fp32 result.
+ *   - block_size is 64 or 128 keys; block n holds the keys [n * block_size,
+ *     (n + 1) * block_size), and a key axis of Skv keys has
+ *     NB = ceil(Skv / block_size) <= EF_MAX_BLOCKS blocks.
+ */
+#define EF_MAX_BLOCKS 16000
+#define EF_MAX_TOPK 256
+
+/*
+ * Summary of the blocks of a key cache: the mean of each block's valid keys,
+ *   summary[b][h][n] = sum over the valid keys j of block n of k[b][h][j] / their number,
+ * and 0 for a block without a valid key. The sum is fp32 and rounded to bf16 once.
+ *   k        : [B][Hkv][Skv][D] bf16;  summary : [B][Hkv][NB][D] bf16.
+ *   new_keys : 0 writes every block. A positive number writes only the blocks that
+ *              hold one of each sequence's last new_keys valid keys, and leaves the
+ *              others as they are: after a decode step appended a key to every
+ *              sequence, new_keys = 1 brings the summaries up to date.
+ * Errors: EF_ERR_INVALID_BLOCKS for block_size, NB or new_keys < 0; others as for
+ * ef_attention_fwd.
+ */
+ef_status ef_block_summary(const void* k, const int* lengths, void* summary, int B, int Hkv,
+                           int Skv, int D, int block_size, int new_keys, void* stream);
+
+/*
+ * Choice of the blocks each query attends to. For query i of sequence b and kv
+ * head h, cur = floor(n_i / block_size) is the query's own block.
+ *   - n_i < 0: no block.  cur + 1 <= topk: the blocks 0 .. cur.
+ *   - Otherwise topk blocks of 0 .. cur: the first sink_blocks, the last
+ *     local_blocks (up to cur, which is always one of them), and of the others
+ *     those with the largest score
+ *       score(n) = max over the Hq/Hkv query heads g of h of <q[b][g][i], summary[b][h][n]>,
+ *     ties to the lower index; a NaN product counts as -inf.
+ * The choice is that of exact arithmetic: where two scores are too close for fp32
+ * to tell apart they are formed again in 64 bits. (Scores beyond the fp32 range
+ * are outside the contract.) The result does not depend on scheduling. A summary
+ * at or behind a query's local blocks is not read, so a partial last block's does
+ * not matter.
+ *   q       : [B][Hq][Sq][D] bf16;  summary : [B][Hkv][NB][D] bf16, NB of Skv keys.
+ *   blocks  : [B][Hkv][Sq][topk] int32: ascending block indices, then -1.
+ *   topk    : 1 .. EF_MAX_TOPK, at least sink_blocks + local_blocks.
+ *   sink_blocks >= 0, local_blocks >= 1.
+ * Errors: EF_ERR_INVALID_BLOCKS for block_size, NB, topk, sink_blocks, local_blocks;
+ * others as for ef_attention_fwd.
+ */
+ef_status ef_block_select(const void* q, const void* summary, const int* lengths, int* blocks,
+                          int B, int Hq, int Hkv, int Sq, int Skv, int D, int block_size,
+                          int topk, int sink_blocks, int local_blocks, void* stream);
 
 #ifdef __cplusplus
 }

@@ -20,3 +20,9 @@ from .attention import (  # noqa: F401
     splitkv_partials_ref,
 )
 from .differential import diff_attention_ref, mixing_weight, rms_norm_rows  # noqa: F401
+from .blocks import (  # noqa: F401
+    attention_blocks_ref,
+    block_select_ref,
+    block_summary_ref,
+    shared_prefix_ref,
+)

@@ -3,51 +3,23 @@
 // grid and workspace arithmetic.
 #include <algorithm>
 #include <cmath>
-#include <cstdint>
 #include <vector>
 
 #include "ef_attention.h"
 #include "ef_device.hpp"
 #include "ef_kernels.hpp"
+#include "host_checks.hpp"
 
 namespace {
+
+using namespace ef::host;
 
 constexpr int kTileKeys = 64;        // key tile of the kernels; partitions are multiples of it
 constexpr int kDecodeMaxRows = 8;    // the VALU split producer handles G*Sq <= 8 ...
 constexpr int kDecodeValuRows = 4;   // ... and the split-KV paths give it G*Sq <= 4 (the MFMA
                                      // producer streams faster with more rows)
-constexpr int kMaxGridYZ = 65535;
 static_assert(ef::kCounterRegionBytes == EF_COUNTER_REGION_BYTES,
               "the counter region of the header is the kernels' one");
-
-struct Shape {
-  int B, Hq, Hkv, Sq, Skv, D;
-  long long rows() const { return (long long)B * Hq * Sq; }
-};
-
-bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-
-ef_status check_shape(const Shape& s) {
-  if (s.B < 0 || s.Sq < 0 || s.Skv < 0 || s.Hq < 1 || s.Hkv < 1) return EF_ERR_INVALID_SHAPE;
-  if (s.Hq % s.Hkv != 0) return EF_ERR_GQA_RATIO;
-  if (s.D != 64 && s.D != 128) return EF_ERR_UNSUPPORTED_HEAD_DIM;
-  // Per-head extents stay below 2^31 elements; batch*heads fits the grid.
-  if ((long long)s.Sq * s.D >= (1LL << 31) || (long long)s.Skv * s.D >= (1LL << 31))
-    return EF_ERR_INVALID_SHAPE;
-  if ((long long)s.B * s.Hkv > kMaxGridYZ || (long long)(s.Hq / s.Hkv) * s.Sq >= (1LL << 31))
-    return EF_ERR_INVALID_SHAPE;
-  return EF_OK;
-}
-
-ef_status check_io(const Shape& s, const void* q, const void* k, const void* v, const float* o,
-                   float scale) {
-  if (!std::isfinite(scale)) return EF_ERR_INVALID_SCALE;
-  if (s.rows() == 0) return EF_OK;
-  if (q == nullptr || o == nullptr) return EF_ERR_NULL_POINTER;
-  if (s.Skv > 0 && (k == nullptr || v == nullptr)) return EF_ERR_NULL_POINTER;
-  if (misaligned(q) || misaligned(o) || misaligned(k) || misaligned(v)) return EF_ERR_MISALIGNED;
-  return EF_OK;
-}
 
 // Visible key runs of a (batch, kv head) for a causal window of `window` keys
 // and `sinks` sink keys (section 7.3). Every key of every query row lies in
@@ -266,8 +238,6 @@ bool fused_combine(const Shape& s, long long P, int d_splits) {
          (long long)s.B * s.Hkv * std::max(d_splits, 1) <= ef::kCounterSlots;
 }
 
-ef_status from_hip(hipError_t e) { return e == hipSuccess ? EF_OK : EF_ERR_HIP; }
-
 // Whether a single-pass launch runs 64-row tiles whose key tiles two groups of
 // waves share (MfmaParams::key_split). A launch with fewer workgroups than the
 // chip holds waits for its longest chain of key tiles, which two groups halve;
@@ -387,6 +357,9 @@ const char* ef_status_string(int status) {
       return "d_splits must be 1, 2 or 4, with at most 8 query rows per kv head";
     case EF_ERR_SCRATCH_TOO_SMALL:
       return "the problem needs more workspace than the library's static scratch holds";
+    case EF_ERR_INVALID_BLOCKS:
+      return "block_size must be 64 or 128 with at most 16000 blocks, topk 1 to 256 and at least "
+             "sink_blocks + local_blocks, sink_blocks >= 0, local_blocks >= 1, new_keys >= 0";
     default: return "unknown status";
   }
 }

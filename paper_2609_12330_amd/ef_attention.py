@@ -33,10 +33,15 @@ STATUS_NAMES = {
     11: "EF_ERR_INVALID_DIFF",
     12: "EF_ERR_INVALID_SPLIT",
     13: "EF_ERR_SCRATCH_TOO_SMALL",
+    14: "EF_ERR_INVALID_BLOCKS",
 }
 
 # Bytes of static scratch behind ef_attention_splitkv_noalloc (EF_STATIC_SCRATCH_BYTES).
 STATIC_SCRATCH_BYTES = 32 << 20
+
+# Limits of block lists (EF_MAX_BLOCKS, EF_MAX_TOPK).
+MAX_BLOCKS = 16000
+MAX_TOPK = 256
 
 # Exported symbols and their C signatures (restype, argtypes).
 _vp, _fp, _i, _f, _sz = ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
@@ -69,6 +74,8 @@ SIGNATURES = {
     "ef_attention_decode_dsplit_workspace_size": (_sz, [_i, _i, _i, _i, _i, _i, _i, _i]),
     "ef_attention_splitkv_noalloc": (_i, [_vp, _vp, _vp, _fp, _i, _i, _i, _i, _i, _i, _f, _i,
                                           _i, _vp]),
+    "ef_block_summary": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp]),
+    "ef_block_select": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _i, _i, _vp]),
 }
 
 
@@ -224,6 +231,17 @@ def ef_attention_splitkv_tune(q, k, v, o, B, Hq, Hkv, Sq, Skv, D, scale, causal,
     return _lib().ef_attention_splitkv_tune(q, k, v, o, B, Hq, Hkv, Sq, Skv, D, scale,
                                             int(causal), window, sinks, workspace,
                                             workspace_bytes, stream, ptr)
+
+
+def ef_block_summary(k, lengths, summary, B, Hkv, Skv, D, block_size, new_keys, stream) -> int:
+    return _lib().ef_block_summary(k, lengths, summary, B, Hkv, Skv, D, block_size, new_keys,
+                                   stream)
+
+
+def ef_block_select(q, summary, lengths, blocks, B, Hq, Hkv, Sq, Skv, D, block_size, topk,
+                    sink_blocks, local_blocks, stream) -> int:
+    return _lib().ef_block_select(q, summary, lengths, blocks, B, Hq, Hkv, Sq, Skv, D, block_size,
+                                  topk, sink_blocks, local_blocks, stream)
 
 
 # ---------------------------------------------------------------------------
@@ -576,3 +594,100 @@ def attention_decode_dsplit(q, k, v, scale: Optional[float] = None, causal: bool
                                     partition_size, ws_ptr, ws_bytes, _stream_handle(stream))
     _check(st, "ef_attention_decode_dsplit")
     return o
+
+
+# ---------------------------------------------------------------------------
+# Long contexts: block-sparse attention and shared prefixes
+# ---------------------------------------------------------------------------
+
+
+def _check_tensor(t, name, dtype, dim, ref=None):
+    """A contiguous GPU tensor of this type and number of axes, on `ref`'s device."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda or (ref is not None and t.device != ref.device):
+        raise TypeError(f"{name} must be a GPU tensor" +
+                        (f" on {ref.device}, got {t.device}" if ref is not None else ""))
+    if t.dim() != dim or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dim}-D tensor")
+
+
+def _lengths_ptr(lengths, B, ref):
+    if lengths is None:
+        return None
+    _check_tensor(lengths, "lengths", _torch().int32, 1, ref)
+    if lengths.shape[0] != B:
+        raise ValueError(f"lengths must have {B} entries, got {lengths.shape[0]}")
+    return lengths.data_ptr()
+
+
+def _call_on(t, stream, fn, *args):
+    """fn(*args, stream handle) with t's device current: a launch needs the device of its
+    stream, and the current stream of another device is not the one t's work is ordered on."""
+    torch = _torch()
+    if stream is not None and stream.device != t.device:
+        raise ValueError(f"stream is on {stream.device}, the tensors are on {t.device}")
+    if torch.cuda.current_device() == t.device.index:
+        return fn(*args, _stream_handle(stream))
+    with torch.cuda.device(t.device):
+        return fn(*args, _stream_handle(stream))
+
+
+def num_blocks(Skv: int, block_size: int = 64) -> int:
+    """Blocks of a key axis of Skv keys."""
+    return -(-Skv // block_size)
+
+
+def block_summary(k, block_size: int = 64, lengths=None, new_keys: int = 0, out=None,
+                  stream=None):
+    """Mean key of every block of k [B, Hkv, Skv, D] through ef_block_summary: bf16
+    [B, Hkv, NB, D]. `lengths` (int32 [B], on the GPU) are the sequences' valid keys. With
+    new_keys > 0 only the blocks of each sequence's last new_keys keys are written, into the
+    `out` that holds the others."""
+    torch = _torch()
+    _check_tensor(k, "k", torch.bfloat16, 4)
+    B, Hkv, Skv, D = k.shape
+    if block_size not in (64, 128):
+        raise ValueError("block_size must be 64 or 128")
+    shape = (B, Hkv, num_blocks(Skv, block_size), D)
+    if out is None:
+        if new_keys:
+            raise ValueError("new_keys needs out, the summaries of the other blocks")
+        out = torch.empty(shape, dtype=torch.bfloat16, device=k.device)
+    else:
+        _check_tensor(out, "out", torch.bfloat16, 4, k)
+        if out.shape != shape:
+            raise ValueError(f"out must be {shape}, got {tuple(out.shape)}")
+    st = _call_on(k, stream, ef_block_summary, k.data_ptr(), _lengths_ptr(lengths, B, k),
+                  out.data_ptr(), B, Hkv, Skv, D, block_size, new_keys)
+    _check(st, "ef_block_summary")
+    return out
+
+
+def block_select(q, summary, Skv: int, topk: int, block_size: int = 64, sink_blocks: int = 1,
+                 local_blocks: int = 1, lengths=None, out=None, stream=None):
+    """The blocks each query of q [B, Hq, Sq, D] attends to, through ef_block_select: int32
+    [B, Hkv, Sq, topk], ascending, filled with -1. summary [B, Hkv, NB, D] is block_summary's
+    for caches of Skv keys."""
+    torch = _torch()
+    _check_tensor(q, "q", torch.bfloat16, 4)
+    _check_tensor(summary, "summary", torch.bfloat16, 4, q)
+    B, Hq, Sq, D = q.shape
+    Hkv = summary.shape[1]
+    if block_size not in (64, 128):
+        raise ValueError("block_size must be 64 or 128")
+    if summary.shape != (B, Hkv, num_blocks(Skv, block_size), D):
+        raise ValueError(f"summary must be [B, Hkv, {num_blocks(Skv, block_size)}, D] matching q, "
+                         f"got {tuple(summary.shape)}")
+    shape = (B, Hkv, Sq, topk)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.int32, device=q.device)
+    else:
+        _check_tensor(out, "out", torch.int32, 4, q)
+        if out.shape != shape:
+            raise ValueError(f"out must be {shape}, got {tuple(out.shape)}")
+    st = _call_on(q, stream, ef_block_select, q.data_ptr(), summary.data_ptr(),
+                  _lengths_ptr(lengths, B, q), out.data_ptr(), B, Hq, Hkv, Sq, Skv, D, block_size,
+                  topk, sink_blocks, local_blocks)
+    _check(st, "ef_block_select")
+    return out

@@ -1,0 +1,109 @@
+"""The long-context entry points on the CPU: every refusal is made on the host before any HIP
+call, and their oracle is pinned by closed forms and by the plain attention oracle."""
+
+import os
+
+import numpy as np
+import pytest
+
+import oracle
+from paper_2609_12330_amd import ef_attention as ef
+
+needs_lib = pytest.mark.skipif(not os.path.exists(ef.LIB_PATH),
+                               reason="libef_attention.so not built")
+
+# Fake device addresses: non-null, 16-byte aligned; never dereferenced on these paths.
+A = 0x10000
+MIS = 0x10008
+
+
+def summary(**kw):
+    a = dict(k=A, n=None, s=A, B=1, Hkv=2, Skv=100, D=128, bs=64, new=0)
+    a.update(kw)
+    return ef.ef_block_summary(a["k"], a["n"], a["s"], a["B"], a["Hkv"], a["Skv"], a["D"],
+                               a["bs"], a["new"], None)
+
+
+def select(**kw):
+    a = dict(q=A, s=A, n=None, o=A, B=1, Hq=4, Hkv=2, Sq=3, Skv=1000, D=128, bs=64, K=8, sinks=1,
+             local=2)
+    a.update(kw)
+    return ef.ef_block_select(a["q"], a["s"], a["n"], a["o"], a["B"], a["Hq"], a["Hkv"], a["Sq"],
+                              a["Skv"], a["D"], a["bs"], a["K"], a["sinks"], a["local"], None)
+
+
+@needs_lib
+@pytest.mark.parametrize("call", [summary, select], ids=["summary", "select"])
+def test_refusals(call):
+    assert call(D=96) == 4
+    assert call(B=-1) == 2
+    assert call(Hkv=0) == 2
+    assert call(Skv=-1) == 2
+    assert call(B=70000) == 2
+    assert call(bs=32) == 14
+    assert call(bs=0) == 14
+    assert call(bs=-64) == 14
+    assert call(Skv=64 * 16000 + 1) == 14
+    assert call(Skv=128 * 16000 + 1, bs=128) == 14
+
+
+@needs_lib
+def test_refusals_of_their_own():
+    assert summary(k=None) == 1
+    assert summary(s=None) == 1
+    assert summary(k=MIS) == 5
+    assert summary(s=MIS) == 5
+    assert summary(new=-1) == 14
+    assert summary(B=0, k=None, s=None) == 0
+    assert summary(Skv=0, k=None, s=None) == 0
+    assert select(Hq=5) == 3
+    assert select(Sq=-1) == 2
+    assert select(q=None) == 1
+    assert select(s=None) == 1
+    assert select(o=None) == 1
+    assert select(q=MIS) == 5
+    assert select(s=MIS) == 5
+    assert select(o=MIS) == 5
+    assert select(K=0) == 14
+    assert select(K=257) == 14
+    assert select(K=2) == 14
+    assert select(sinks=-1) == 14
+    assert select(local=0) == 14
+    assert select(sinks=2**31 - 1, local=2**31 - 1) == 14
+    assert select(Sq=0, q=None, o=None) == 0
+    assert ef.library().ef_status_string(14) != b"unknown status"
+
+
+def test_oracle_summary_and_selection():
+    k = np.arange(10.0).reshape(1, 1, 10, 1) * np.ones((1, 1, 10, 3))
+    m = oracle.block_summary_ref(k, 4, [9])
+    assert np.array_equal(m[0, 0, :, 0], [1.5, 5.5, 8.0])
+    assert np.array_equal(oracle.block_summary_ref(k, 4, [0]), np.zeros((1, 1, 3, 3)))
+    # Six blocks of four keys, one head pair; the score of a block is its larger product.
+    q = np.array([[1.0, 0.0], [0.0, 1.0]]).reshape(1, 2, 1, 2)
+    s = np.array([[0, 0], [3, -9], [1, 3], [2, 2], [5, 5], [0, 0]], float).reshape(1, 1, 6, 2)
+    assert oracle.block_select_ref(q, s, 24, 3, 4, 1, 1).tolist() == [[[[0, 4, 5]]]]
+    assert oracle.block_select_ref(q, s, 24, 4, 4, 1, 1).tolist() == [[[[0, 1, 4, 5]]]]  # tie: 1
+    assert oracle.block_select_ref(q, s, 24, 3, 4, 0, 1, [9]).tolist() == [[[[0, 1, 2]]]]
+    assert oracle.block_select_ref(q, s, 24, 3, 4, 1, 2, [20]).tolist() == [[[[0, 3, 4]]]]
+    assert oracle.block_select_ref(q, s, 24, 3, 4, 1, 2, [0]).tolist() == [[[[-1, -1, -1]]]]
+
+
+def test_oracle_attention_agrees_with_the_plain_one():
+    rng = np.random.default_rng(0)
+    B, Hq, H, Sq, S, Lp, D = 2, 4, 2, 5, 37, 19, 64
+    q, k, v = (rng.standard_normal((B, h, n, D)) for h, n in ((Hq, Sq), (H, S), (H, S)))
+    every = np.broadcast_to(np.arange(3), (B, H, Sq, 3))
+    full = oracle.attention_ref(q, k, v, 0.2, True)
+    assert np.allclose(oracle.attention_blocks_ref(q, k, v, every, 16, 0.2), full, atol=1e-12)
+    assert np.array_equal(
+        oracle.attention_blocks_ref(q, k, v, np.full((B, H, Sq, 2), -1), 16, 0.2), 0 * q)
+    kp, vp = (rng.standard_normal((H, Lp, D)) for _ in range(2))
+    kk = np.concatenate([np.broadcast_to(kp, (B, H, Lp, D)), k], 2)
+    vv = np.concatenate([np.broadcast_to(vp, (B, H, Lp, D)), v], 2)
+    for causal in (False, True):
+        assert np.allclose(oracle.shared_prefix_ref(q, kp, vp, k, v, 0.2, causal),
+                           oracle.attention_ref(q, kk, vv, 0.2, causal), atol=1e-12)
+    short = oracle.shared_prefix_ref(q, kp, vp, k, v, 0.2, True, [30, 2])
+    assert np.allclose(short[0], oracle.attention_ref(q[:1], kk[:1, :, :49], vv[:1, :, :49], 0.2,
+                                                      True)[0], atol=1e-12)
