@@ -475,6 +475,56 @@ ef_status ef_block_select(const void* q, const void* summary, const int* lengths
                           int B, int Hq, int Hkv, int Sq, int Skv, int D, int block_size,
                           int topk, int sink_blocks, int local_blocks, void* stream);
 
+/*
+ * Attention over selected blocks: query i of sequence b and query head hq sees the
+ * keys j <= n_i whose block is in the list of (b, hq / (Hq/Hkv), i). A row without a
+ * visible key gets 0.
+ *   blocks : [B][Hkv][Sq][topk] int32, 16-byte aligned, as ef_block_select writes it
+ *            or any other choice: the order does not matter, an entry outside
+ *            0 .. floor(n_i / block_size) is passed over, a repeated one counts once.
+ *   topk   : 1 .. EF_MAX_TOPK.
+ *   o      : [B][Hq][Sq][D] bf16.
+ *   workspace : ef_attention_blocks_workspace_size(...) bytes, 16-byte aligned (may
+ *            be NULL where that is 0). It holds partial states during the call only
+ *            and need not be cleared; calls that overlap in time must not share one,
+ *            and neither must two captured graphs that may run at the same time.
+ * Work and traffic grow with the union of the lists of about 64 * Hkv / Hq neighbouring
+ * queries, which is little more than one list where neighbours choose alike.
+ * Errors: EF_ERR_INVALID_BLOCKS for block_size, NB or topk; others as for
+ * ef_attention_splitkv.
+ */
+ef_status ef_attention_blocks(const void* q, const void* k, const void* v, const int* blocks,
+                              const int* lengths, void* o, int B, int Hq, int Hkv, int Sq,
+                              int Skv, int D, float scale, int block_size, int topk,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of ef_attention_blocks; 0 for invalid arguments too. */
+size_t ef_attention_blocks_workspace_size(int B, int Hq, int Hkv, int Sq, int Skv, int D,
+                                          int block_size, int topk);
+
+/*
+ * Attention of a batch over one shared prefix: the keys of sequence b are the Lp keys
+ * of the prefix, the same for all sequences, followed by its len_b own ones. With
+ * causal != 0 query i sees the keys up to its own place, Lp + n_i, of this
+ * concatenation (a place before its first key: none, and the row is 0); otherwise it
+ * sees them all. Each prefix key is read once for the rows of all sequences.
+ *   k_prefix, v_prefix : [Hkv][Lp][D] bf16;  k, v : [B][Hkv][Skv][D] bf16.
+ *   o         : [B][Hq][Sq][D] bf16.
+ *   Lp, Skv   : either may be 0.
+ *   workspace : as for ef_attention_blocks, ef_attention_shared_prefix_workspace_size(...)
+ *               bytes.
+ * Errors as for ef_attention_splitkv.
+ */
+ef_status ef_attention_shared_prefix(const void* q, const void* k_prefix, const void* v_prefix,
+                                     const void* k, const void* v, const int* lengths, void* o,
+                                     int B, int Hq, int Hkv, int Sq, int Lp, int Skv, int D,
+                                     float scale, int causal, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of ef_attention_shared_prefix; 0 for invalid arguments too. */
+size_t ef_attention_shared_prefix_workspace_size(int B, int Hq, int Hkv, int Sq, int Lp, int Skv,
+                                                 int D);
+
 #ifdef __cplusplus
 }
 #endif

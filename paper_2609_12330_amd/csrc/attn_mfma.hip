@@ -585,6 +585,7 @@ void attn_mfma_kernel(MfmaParams a) {
     floatx16 xa, xb;        // scores of odd and even subtiles
     uint32_t pa[8], pb[8];  // their weights
     Rolling<D> ro{kread, vread, qf, oacc, lsum, mref, c};
+    const KeyMask mask{lim, lo, tl.sinks, h};
     if (ntiles > 0) {
       StageLoader<D, NW, NV> ld;
       ld.init(kh, vh, wave, DIFF ? wid : wave);
@@ -618,14 +619,14 @@ void attn_mfma_kernel(MfmaParams a) {
         t2 = tile(u + 2);
         if (GROUPS == 1 || 2 * u + 1 < nsub)
           pair_step<D, NW, NV, RENEW>(k1, k0, v0, v1, ro, ld, t0, t1, t2, 2 * u + 2 < nsub, top,
-                                      lim, lo, tl.sinks, h, xa, xb, pa, pb);
+                                      mask, xa, xb, pa, pb);
         wait_tile_loads();
         __syncthreads();
         if (u + 1 >= steps) break;
         t0 = tile(u + 3);
         if (GROUPS == 1 || 2 * u + 3 < nsub)
           pair_step<D, NW, NV, RENEW>(k0, k1, v1, v0, ro, ld, t1, t2, t0, 2 * u + 4 < nsub, top,
-                                      lim, lo, tl.sinks, h, xa, xb, pa, pb);
+                                      mask, xa, xb, pa, pb);
         wait_tile_loads();
         __syncthreads();
         t1 = t0;

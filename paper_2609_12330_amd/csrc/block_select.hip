@@ -19,7 +19,7 @@
 // is the exact one. Elsewhere only the blocks within 2 E of the border are scored
 // again in 64 bits (products of bf16 are exact there and their sum is to 2^-53),
 // in index order, and the best of them complete the list.
-#include "ef_blocks.hpp"
+#include "ef_long.hpp"
 #include "ef_device.hpp"
 
 namespace ef {

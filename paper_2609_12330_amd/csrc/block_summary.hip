@@ -6,7 +6,7 @@
 // load covers 512 / D whole keys and all loads of 64 keys are in flight before
 // the first is used. The lanes that hold the same chunk of other keys meet in
 // registers (DPP and lane swaps), and the first D / 8 lanes store the row.
-#include "ef_blocks.hpp"
+#include "ef_long.hpp"
 #include "ef_device.hpp"
 
 namespace ef {

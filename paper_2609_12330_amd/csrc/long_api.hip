@@ -1,0 +1,327 @@
+// Host side of the long-context entry points of include/ef_attention.h: argument
+// validation, launch shapes and workspace arithmetic.
+#include <algorithm>
+#include <cmath>
+
+#include "ef_attention.h"
+#include "ef_long.hpp"
+#include "ef_device.hpp"
+#include "host_checks.hpp"
+
+namespace {
+
+using namespace ef::host;
+
+static_assert(ef::kMaxBlocks == EF_MAX_BLOCKS && ef::kMaxTopk == EF_MAX_TOPK,
+              "the limits of the header are the kernels' ones");
+
+// Blocks of a key axis, or -1 where block_size or their number is refused.
+int num_blocks(int Skv, int block_size) {
+  if (block_size != 64 && block_size != 128) return -1;
+  const int nb = (int)(((long long)Skv + block_size - 1) / block_size);
+  return nb <= ef::kMaxBlocks ? nb : -1;
+}
+
+// Most bytes of LDS a selection workgroup keeps its scores in: two workgroups to
+// a compute unit, and any list of EF_MAX_BLOCKS scores fits.
+constexpr int kSelectLds = 64 * 1024 - 256;
+
+}  // namespace
+
+extern "C" {
+
+ef_status ef_block_summary(const void* k, const int* lengths, void* summary, int B, int Hkv,
+                           int Skv, int D, int block_size, int new_keys, void* stream) {
+  const Shape s{B, Hkv, Hkv, 1, Skv, D};
+  const ef_status st = check_shape(s);
+  if (st != EF_OK) return st;
+  const int nb = num_blocks(Skv, block_size);
+  if (nb < 0 || new_keys < 0) return EF_ERR_INVALID_BLOCKS;
+  if (B == 0 || nb == 0) return EF_OK;
+  if (k == nullptr || summary == nullptr) return EF_ERR_NULL_POINTER;
+  if (misaligned(k) || misaligned(summary)) return EF_ERR_MISALIGNED;
+  ef::SummaryParams a{};
+  a.k = static_cast<const uint16_t*>(k);
+  a.lengths = lengths;
+  a.s = static_cast<uint16_t*>(summary);
+  a.B = B; a.Hkv = Hkv; a.Skv = Skv; a.D = D;
+  a.NB = nb;
+  a.block = block_size;
+  a.new_keys = new_keys;
+  // The last new_keys keys lie in at most this many blocks.
+  a.touched = new_keys == 0
+                  ? nb
+                  : (int)std::min<long long>(nb, ((long long)new_keys + block_size - 2) /
+                                                         block_size + 1);
+  return from_hip(ef::launch_block_summary(a, static_cast<hipStream_t>(stream)));
+}
+
+ef_status ef_block_select(const void* q, const void* summary, const int* lengths, int* blocks,
+                          int B, int Hq, int Hkv, int Sq, int Skv, int D, int block_size,
+                          int topk, int sink_blocks, int local_blocks, void* stream) {
+  const Shape s{B, Hq, Hkv, Sq, Skv, D};
+  const ef_status st = check_shape(s);
+  if (st != EF_OK) return st;
+  const int nb = num_blocks(Skv, block_size);
+  if (nb < 0 || topk < 1 || topk > ef::kMaxTopk || sink_blocks < 0 || local_blocks < 1 ||
+      (long long)sink_blocks + local_blocks > topk)
+    return EF_ERR_INVALID_BLOCKS;
+  if (s.rows() == 0) return EF_OK;
+  if (q == nullptr || blocks == nullptr || (nb > 0 && summary == nullptr))
+    return EF_ERR_NULL_POINTER;
+  if (misaligned(q) || misaligned(summary) || misaligned(blocks)) return EF_ERR_MISALIGNED;
+  ef::SelectParams a{};
+  a.q = static_cast<const uint16_t*>(q);
+  a.s = static_cast<const uint16_t*>(summary);
+  a.lengths = lengths;
+  a.out = blocks;
+  a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.Sq = Sq; a.Skv = Skv; a.D = D;
+  a.G = Hq / Hkv;
+  a.NB = nb;
+  a.shift = block_size == 64 ? 6 : 7;
+  a.K = topk;
+  a.sinks = sink_blocks;
+  a.local = local_blocks;
+  a.gp = 1;
+  while (a.gp < a.G && a.gp < 16) a.gp *= 2;
+  a.per = (a.G + 15) / 16;
+  // Rows of four floats more than whole tiles: 16 positions' rows start in different banks.
+  a.stride = (nb + 15) / 16 * 16 + 4;
+  // Positions per workgroup: four column tiles where the scores fit and the grid
+  // still fills the chip, else one tile, fewer positions where they do not fit.
+  const long long heads = (long long)B * Hkv;
+  const int fit = std::max(1, kSelectLds / (a.stride * 4));
+  int pos = a.per > 1 ? 1 : 16 / a.gp;
+  if (a.per == 1 && 4 * pos <= fit && heads * ((Sq + 4 * pos - 1) / (4 * pos)) >= 512) pos *= 4;
+  a.pos = std::min(std::min(pos, fit), Sq);
+  const long long ptiles = ((long long)Sq + a.pos - 1) / a.pos;
+  if (heads * ptiles >= (1LL << 31)) return EF_ERR_INVALID_SHAPE;
+  a.ptiles = (int)ptiles;
+  return from_hip(ef::launch_block_select(a, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
+
+namespace {
+
+// m, l [rows][P] and acc [rows][P][D] of a workspace of partial states.
+struct StateLayout {
+  size_t l_off, acc_off, bytes;
+};
+
+StateLayout state_layout(long long rows, long long P, int D) {
+  StateLayout w;
+  w.l_off = ef::ws_align256((size_t)(rows * P) * sizeof(float));
+  w.acc_off = 2 * w.l_off;
+  w.bytes = w.acc_off + (size_t)(rows * P) * D * sizeof(float);
+  return w;
+}
+
+template <class Params>
+void set_states(Params& a, const StateLayout& w, void* workspace) {
+  char* ws = static_cast<char*>(workspace);
+  a.ws_m = reinterpret_cast<float*>(ws);
+  a.ws_l = reinterpret_cast<float*>(ws + w.l_off);
+  a.ws_acc = reinterpret_cast<float*>(ws + w.acc_off);
+}
+
+template <class Params>
+ef_status combine_states(const Params& a, long long rows, hipStream_t stream) {
+  ef::StateCombineParams c{};
+  c.m = a.ws_m;
+  c.l = a.ws_l;
+  c.acc = a.ws_acc;
+  c.o = a.o;
+  c.rows = (int)rows;
+  c.P = a.P;
+  c.D = a.D;
+  return from_hip(ef::launch_state_combine(c, stream));
+}
+
+// Workgroups that fill the chip: two of the matrix-core kernels fit on a compute unit.
+constexpr long long kFillWgs = 512;
+
+// Launch shape of attention over selected blocks. The rows of a kv head are cut into
+// tiles of `bm`; where these are few, P workgroups share a tile's blocks.
+struct BlocksPlan {
+  int bm, mtiles, P;
+};
+
+BlocksPlan blocks_plan(const Shape& s, int nb, int topk) {
+  BlocksPlan p;
+  const long long R = (long long)(s.Hq / s.Hkv) * s.Sq;
+  p.bm = 64;
+  p.mtiles = (int)((R + p.bm - 1) / p.bm);
+  const long long groups = (long long)s.B * s.Hkv * p.mtiles;
+  const long long most = std::max(1, std::min(std::min(nb, topk), 64));
+  p.P = (int)std::min(std::max(kFillWgs / std::max(groups, 1LL), 1LL), most);
+  return p;
+}
+
+ef_status check_blocks(const Shape& s, int block_size, int topk) {
+  const ef_status st = check_shape(s);
+  if (st != EF_OK) return st;
+  if (num_blocks(s.Skv, block_size) < 0 || topk < 1 || topk > ef::kMaxTopk)
+    return EF_ERR_INVALID_BLOCKS;
+  return s.rows() < (1LL << 31) ? EF_OK : EF_ERR_INVALID_SHAPE;
+}
+
+// Launch shape of attention over a shared prefix: see PrefixParams.
+struct PrefixPlan {
+  bool whole;
+  int P1, T1, mt1, P2, T2, mt2, P;
+  long long n_prefix, n_own;
+};
+
+constexpr int kPrefixRows = 128;
+
+// `tiles` tiles in about `parts` parts of at least `least` tiles: tiles per part.
+int tiles_per_part(long long tiles, long long parts, int least) {
+  const long long p = std::max(parts, 1LL);
+  return (int)std::max<long long>((tiles + p - 1) / p, std::min<long long>(least, tiles));
+}
+
+PrefixPlan prefix_plan(const Shape& s, int Lp) {
+  PrefixPlan p{};
+  const long long R = (long long)(s.Hq / s.Hkv) * s.Sq, heads = (long long)s.B * s.Hkv;
+  const long long np = (Lp + 63) / 64, no = ((long long)s.Skv + 63) / 64;
+  p.mt1 = (int)((s.B * R + kPrefixRows - 1) / kPrefixRows);
+  p.mt2 = (int)((R + kPrefixRows - 1) / kPrefixRows);
+  p.whole = np + no == 0 || (R >= 64 && heads * p.mt2 >= 192);
+  if (p.whole) {
+    p.P2 = p.P = 1;
+    p.n_own = heads * p.mt2;
+    return p;
+  }
+  if (np > 0) {
+    p.T1 = tiles_per_part(np, kFillWgs / 2 / (s.Hkv * (long long)p.mt1), 2);
+    p.P1 = (int)((np + p.T1 - 1) / p.T1);
+    p.n_prefix = (long long)s.Hkv * p.mt1 * p.P1;
+  }
+  if (no > 0) {
+    p.T2 = tiles_per_part(no, kFillWgs / (heads * p.mt2), 4);
+    p.P2 = (int)((no + p.T2 - 1) / p.T2);
+    p.n_own = heads * p.mt2 * p.P2;
+  }
+  p.P = p.P1 + p.P2;
+  return p;
+}
+
+ef_status check_prefix(const Shape& s, int Lp) {
+  const ef_status st = check_shape(s);
+  if (st != EF_OK) return st;
+  if (Lp < 0 || (long long)Lp * s.D >= (1LL << 31)) return EF_ERR_INVALID_SHAPE;
+  // Rows are counted over the whole batch.
+  return s.rows() < (1LL << 31) ? EF_OK : EF_ERR_INVALID_SHAPE;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ef_attention_blocks_workspace_size(int B, int Hq, int Hkv, int Sq, int Skv, int D,
+                                          int block_size, int topk) {
+  const Shape s{B, Hq, Hkv, Sq, Skv, D};
+  if (check_blocks(s, block_size, topk) != EF_OK || s.rows() == 0) return 0;
+  const BlocksPlan p = blocks_plan(s, num_blocks(Skv, block_size), topk);
+  return p.P == 1 ? 0 : state_layout(s.rows(), p.P, D).bytes;
+}
+
+ef_status ef_attention_blocks(const void* q, const void* k, const void* v, const int* blocks,
+                              const int* lengths, void* o, int B, int Hq, int Hkv, int Sq,
+                              int Skv, int D, float scale, int block_size, int topk,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  const Shape s{B, Hq, Hkv, Sq, Skv, D};
+  ef_status st = check_blocks(s, block_size, topk);
+  if (st != EF_OK) return st;
+  st = check_io(s, q, k, v, o, scale);
+  if (st != EF_OK) return st;
+  if (s.rows() == 0) return EF_OK;
+  if (blocks == nullptr) return EF_ERR_NULL_POINTER;
+  if (misaligned(blocks)) return EF_ERR_MISALIGNED;
+  const BlocksPlan p = blocks_plan(s, num_blocks(Skv, block_size), topk);
+  ef::BlocksParams a{};
+  if (p.P > 1) {
+    const StateLayout w = state_layout(s.rows(), p.P, D);
+    if (workspace == nullptr || workspace_bytes < w.bytes) return EF_ERR_WORKSPACE_TOO_SMALL;
+    if (misaligned(workspace)) return EF_ERR_MISALIGNED;
+    set_states(a, w, workspace);
+  }
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.blocks = blocks;
+  a.lengths = lengths;
+  a.o = static_cast<uint16_t*>(o);
+  a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.Sq = Sq; a.Skv = Skv; a.D = D;
+  a.G = Hq / Hkv;
+  a.R = a.G * Sq;
+  a.NB = num_blocks(Skv, block_size);
+  a.shift = block_size == 64 ? 6 : 7;
+  a.K = topk;
+  a.P = p.P;
+  a.bm = p.bm;
+  a.mtiles = p.mtiles;
+  a.c_abs = std::fabs(scale) * ef::kLog2e;
+  a.qflip = scale < 0.f ? 0x80008000u : 0u;
+  if ((long long)B * Hkv * p.mtiles * p.P >= (1LL << 31)) return EF_ERR_INVALID_SHAPE;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  st = from_hip(ef::launch_attention_blocks(a, hs));
+  return st != EF_OK || p.P == 1 ? st : combine_states(a, s.rows(), hs);
+}
+
+size_t ef_attention_shared_prefix_workspace_size(int B, int Hq, int Hkv, int Sq, int Lp, int Skv,
+                                                 int D) {
+  const Shape s{B, Hq, Hkv, Sq, Skv, D};
+  if (check_prefix(s, Lp) != EF_OK || s.rows() == 0) return 0;
+  const PrefixPlan p = prefix_plan(s, Lp);
+  return p.P == 1 ? 0 : state_layout(s.rows(), p.P, D).bytes;
+}
+
+ef_status ef_attention_shared_prefix(const void* q, const void* k_prefix, const void* v_prefix,
+                                     const void* k, const void* v, const int* lengths, void* o,
+                                     int B, int Hq, int Hkv, int Sq, int Lp, int Skv, int D,
+                                     float scale, int causal, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  const Shape s{B, Hq, Hkv, Sq, Skv, D};
+  ef_status st = check_prefix(s, Lp);
+  if (st != EF_OK) return st;
+  st = check_io(s, q, k, v, o, scale);
+  if (st != EF_OK) return st;
+  if (s.rows() == 0) return EF_OK;
+  if (Lp > 0 && (k_prefix == nullptr || v_prefix == nullptr)) return EF_ERR_NULL_POINTER;
+  if (misaligned(k_prefix) || misaligned(v_prefix)) return EF_ERR_MISALIGNED;
+  const PrefixPlan p = prefix_plan(s, Lp);
+  ef::PrefixParams a{};
+  if (p.P > 1) {
+    const StateLayout w = state_layout(s.rows(), p.P, D);
+    if (workspace == nullptr || workspace_bytes < w.bytes) return EF_ERR_WORKSPACE_TOO_SMALL;
+    if (misaligned(workspace)) return EF_ERR_MISALIGNED;
+    set_states(a, w, workspace);
+  }
+  a.q = static_cast<const uint16_t*>(q);
+  a.kp = static_cast<const uint16_t*>(k_prefix);
+  a.vp = static_cast<const uint16_t*>(v_prefix);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.lengths = lengths;
+  a.o = static_cast<uint16_t*>(o);
+  a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.Sq = Sq; a.Skv = Skv; a.Lp = Lp; a.D = D;
+  a.G = Hq / Hkv;
+  a.R = a.G * Sq;
+  a.causal = causal ? 1 : 0;
+  a.whole = p.whole ? 1 : 0;
+  a.P1 = p.P1; a.T1 = p.T1; a.mt1 = p.mt1;
+  a.P2 = p.P2; a.T2 = p.T2; a.mt2 = p.mt2;
+  a.P = p.P;
+  if (p.n_prefix + p.n_own >= (1LL << 31)) return EF_ERR_INVALID_SHAPE;
+  a.n_prefix = (unsigned)p.n_prefix;
+  a.n_own = (unsigned)p.n_own;
+  a.c_abs = std::fabs(scale) * ef::kLog2e;
+  a.qflip = scale < 0.f ? 0x80008000u : 0u;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  st = from_hip(ef::launch_attention_prefix(a, hs));
+  return st != EF_OK || p.P == 1 ? st : combine_states(a, s.rows(), hs);
+}
+
+}  // extern "C"

@@ -122,9 +122,14 @@ __device__ __forceinline__ void static_for(F&& f) {
 // 64 rows per wave, one wave per SIMD (half the fragment reads, 2.1 GHz, 51%
 // busy: 952 and 171 us); three or four stages per tile (25 us against 20 on a
 // 777-token prompt).
-template <int D>
+//
+// With SEL a tile may be hidden from single rows as a whole (a block that other rows
+// of the workgroup selected): select() sets the offset of such a row's exponents to
+// -inf, so its weights are 0 at the cost of one instruction a subtile.
+template <int D, bool SEL = false>
 struct Rolling {
   using Geo = TileGeom<D>;
+  static constexpr bool SELECTS = SEL;
   static constexpr int KSTEPS = D / 16;
   static constexpr int DT = D / 32;
   static constexpr int NV = 2 * DT;            // value products of a subtile
@@ -153,6 +158,20 @@ struct Rolling {
   float& lsum;
   float& mref;
   float c;
+  bool on = true;     // SEL: whether this lane's row sees the tile
+  float bias = 0.f;   // SEL: -reference, or -inf where it does not
+
+  __device__ __forceinline__ void select(bool sees) {
+    on = sees;
+    rebias();
+  }
+  __device__ __forceinline__ void rebias() {
+    if constexpr (SEL) bias = on ? -mref : kNegInf;
+  }
+  // The largest score of a row counts for its reference only where the row sees it.
+  __device__ __forceinline__ float seen(float cand) const {
+    return !SEL || on ? cand : kNegInf;
+  }
 
   // Fragment of product i of a subtile, K and V subtiles at kt and vt.
   template <int I>
@@ -205,7 +224,7 @@ struct Rolling {
     constexpr int lo = 16 * I / N, hi = 16 * (I + 1) / N;
     static_for<hi - lo>([&](auto q) {
       constexpr int e = lo + decltype(q)::value;
-      const float p = exp2_fast(fmaf(x[e], c, -mref));
+      const float p = exp2_fast(fmaf(x[e], c, SEL ? bias : -mref));
       if constexpr (e % 2 == 0) {
         f.prev = p;
       } else {
@@ -226,10 +245,18 @@ struct Rolling {
   // longer exactly 1 but rounded to bf16: the error against 64 bits of 64 keys at
   // D = 64 was 1.50e-3 instead of 1.33e-3, of 384 keys 1.62e-3 instead of 1.60e-3.
   __device__ __forceinline__ void start(const floatx16& x0, const floatx16& x1, uint32_t* pout) {
-    mref = fmaxf(mref, tile_max(x0, x1));
+    mref = fmaxf(mref, seen(tile_max(x0, x1)));
+    rebias();
     Soft f;
     soft_slot<0, 1>(f, x0, pout);
     lsum += (f.ps[0] + f.ps[1]) + (f.ps[2] + f.ps[3]);
+  }
+  // start() of a loop that carries a state from an earlier one.
+  __device__ __forceinline__ void resume(const floatx16& x0, const floatx16& x1, uint32_t* pout) {
+    const float old = mref;
+    mref = fmaxf(mref, seen(tile_max(x0, x1)));
+    rescale(exp2_fast(old - mref));
+    start(x0, x1, pout);
   }
   // A tile that renews the reference: it moves to the maximum of the tile, down as
   // well as up, and the carried sum and value move with it. Down at most
@@ -270,7 +297,8 @@ struct Rolling {
       for (int i = 2; i < 16; ++i) tmax = fmaxf(tmax, x[i]);
       const float cand = max_with_other_half(tmax) * c;
       const float old = mref;
-      mref = fmaxf(mref, cand);
+      mref = fmaxf(mref, seen(cand));
+      rebias();
       rescale(exp2_fast(old - mref));  // by 1 where the reference stayed
       soft_slot<0, 1>(f, x, pout);
       sum = (f.ps[0] + f.ps[1]) + (f.ps[2] + f.ps[3]);
@@ -422,42 +450,62 @@ struct StageLoader {
   }
 };
 
-// One step of the rolling loop, tiles t0 = u, t1 = u + 1, t2 = u + 2: the softmax
-// of the second half of tile u (scores in xa) and of the first half of tile u + 1
-// (xb, if `second`), beside the scores of tile u + 1 (K stage `knext`) and the
-// values of tile u (V stage `vcur`, weights of its first half in pb on entry).
-// Meanwhile K of tile u + 2 and V of tile u + 1 land in the two stages nobody
-// reads during the step. With RENEW a tile u + 1 may renew the reference: then its
-// weights wait for both halves of its scores and all values of tile u.
-template <int D, int NW, int NV, bool RENEW>
-__device__ __forceinline__ void pair_step(char* knext, char* kfree, char* vcur, char* vfree,
-                                          Rolling<D>& ro, const StageLoader<D, NW, NV>& ld,
-                                          const TileAt& t0, TileAt& t1, const TileAt& t2,
-                                          bool second, float& top, int lim, int lo, int sinks,
-                                          int h, floatx16& xa, floatx16& xb, uint32_t* pa,
-                                          uint32_t* pb) {
-  using R = Rolling<D>;
+// Visibility of keys to this lane's row inside a tile (see mask_scores).
+struct KeyMask {
+  int lim, lo, sinks, h;
+  __device__ __forceinline__ void operator()(floatx16& x, int kb, int kend) const {
+    mask_scores(x, kb, kend, lim, lo, sinks, h);
+  }
+};
+
+// The products and the softmax of one step of the rolling loop, tiles t0 = u, t1 =
+// u + 1: the softmax of the second half of tile u (scores in xa) and of the first
+// half of tile u + 1 (xb, if `second`), beside the scores of tile u + 1 (K stage
+// `knext`) and the values of tile u (V stage `vcur`, weights of its first half in pb
+// on entry). With RENEW a tile u + 1 may renew the reference: then its weights wait
+// for both halves of its scores and all values of tile u. on0, on1: whether this
+// lane's row sees the tiles at all (a loop that selects).
+template <int D, bool RENEW, class Ro>
+__device__ __forceinline__ void pair_compute(char* knext, char* vcur, Ro& ro, const TileAt& t0,
+                                             TileAt& t1, bool second, float& top,
+                                             const KeyMask& mask, floatx16& xa, floatx16& xb,
+                                             uint32_t* pa, uint32_t* pb, bool on0 = true,
+                                             bool on1 = true) {
   constexpr int SUB = TileGeom<D>::SUB;
-  u32x4_t carry[R::PF];
-  ld.template load<true>(kfree, t2.base, t2.end);
-  ld.template load<false>(vfree, t1.base, t1.end);
-  if (t0.masked) mask_scores(xa, t0.base + 32, t0.end, lim, lo, sinks, h);
+  u32x4_t carry[Ro::PF];
+  if (t0.masked) mask(xa, t0.base + 32, t0.end);
+  if constexpr (Ro::SELECTS) ro.select(on0);
   ro.template subtile<false, true>(xa, xb, pb, pa, knext, vcur, knext + SUB, vcur + SUB, carry);
   const bool renews = RENEW && __builtin_expect(t1.renews, 0);
   if (second && !renews) {
-    if (t1.masked) mask_scores(xb, t1.base, t1.end, lim, lo, sinks, h);
+    if (t1.masked) mask(xb, t1.base, t1.end);
+    if constexpr (Ro::SELECTS) ro.select(on1);
     ro.template subtile<true, false>(xb, xa, pa, pb, knext + SUB, vcur + SUB, nullptr, nullptr,
                                      carry);
   }
   if (renews) {
     ro.products(xa, pa, knext + SUB, vcur + SUB);
     if (t1.masked) {
-      mask_scores(xb, t1.base, t1.end, lim, lo, sinks, h);
-      mask_scores(xa, t1.base + 32, t1.end, lim, lo, sinks, h);
+      mask(xb, t1.base, t1.end);
+      mask(xa, t1.base + 32, t1.end);
       t1.masked = false;  // both halves are
     }
     ro.renew(top, xb, xa, pb);
   }
+}
+
+// One step of the rolling loop: pair_compute while K of tile t2 = u + 2 and V of tile
+// u + 1 land in the two stages nobody reads during the step.
+template <int D, int NW, int NV, bool RENEW>
+__device__ __forceinline__ void pair_step(char* knext, char* kfree, char* vcur, char* vfree,
+                                          Rolling<D>& ro, const StageLoader<D, NW, NV>& ld,
+                                          const TileAt& t0, TileAt& t1, const TileAt& t2,
+                                          bool second, float& top, const KeyMask& mask,
+                                          floatx16& xa, floatx16& xb, uint32_t* pa,
+                                          uint32_t* pb) {
+  ld.template load<true>(kfree, t2.base, t2.end);
+  ld.template load<false>(vfree, t1.base, t1.end);
+  pair_compute<D, RENEW>(knext, vcur, ro, t0, t1, second, top, mask, xa, xb, pa, pb);
 }
 
 }  // namespace ef

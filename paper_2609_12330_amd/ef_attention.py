@@ -76,6 +76,12 @@ SIGNATURES = {
                                           _i, _vp]),
     "ef_block_summary": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp]),
     "ef_block_select": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _i, _i, _vp]),
+    "ef_attention_blocks": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _f, _i, _i,
+                                 _vp, _sz, _vp]),
+    "ef_attention_blocks_workspace_size": (_sz, [_i, _i, _i, _i, _i, _i, _i, _i]),
+    "ef_attention_shared_prefix": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i,
+                                        _i, _f, _i, _vp, _sz, _vp]),
+    "ef_attention_shared_prefix_workspace_size": (_sz, [_i, _i, _i, _i, _i, _i, _i]),
 }
 
 
@@ -242,6 +248,27 @@ def ef_block_select(q, summary, lengths, blocks, B, Hq, Hkv, Sq, Skv, D, block_s
                     sink_blocks, local_blocks, stream) -> int:
     return _lib().ef_block_select(q, summary, lengths, blocks, B, Hq, Hkv, Sq, Skv, D, block_size,
                                   topk, sink_blocks, local_blocks, stream)
+
+
+def ef_attention_blocks(q, k, v, blocks, lengths, o, B, Hq, Hkv, Sq, Skv, D, scale, block_size,
+                        topk, workspace, workspace_bytes, stream) -> int:
+    return _lib().ef_attention_blocks(q, k, v, blocks, lengths, o, B, Hq, Hkv, Sq, Skv, D, scale,
+                                      block_size, topk, workspace, workspace_bytes, stream)
+
+
+def ef_attention_blocks_workspace_size(B, Hq, Hkv, Sq, Skv, D, block_size, topk) -> int:
+    return _lib().ef_attention_blocks_workspace_size(B, Hq, Hkv, Sq, Skv, D, block_size, topk)
+
+
+def ef_attention_shared_prefix(q, k_prefix, v_prefix, k, v, lengths, o, B, Hq, Hkv, Sq, Lp, Skv,
+                               D, scale, causal, workspace, workspace_bytes, stream) -> int:
+    return _lib().ef_attention_shared_prefix(q, k_prefix, v_prefix, k, v, lengths, o, B, Hq, Hkv,
+                                             Sq, Lp, Skv, D, scale, int(causal), workspace,
+                                             workspace_bytes, stream)
+
+
+def ef_attention_shared_prefix_workspace_size(B, Hq, Hkv, Sq, Lp, Skv, D) -> int:
+    return _lib().ef_attention_shared_prefix_workspace_size(B, Hq, Hkv, Sq, Lp, Skv, D)
 
 
 # ---------------------------------------------------------------------------
@@ -691,3 +718,94 @@ def block_select(q, summary, Skv: int, topk: int, block_size: int = 64, sink_blo
                   topk, sink_blocks, local_blocks)
     _check(st, "ef_block_select")
     return out
+
+
+def _out_bf16(q, out):
+    torch = _torch()
+    if out is None:
+        return torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    _check_tensor(out, "out", torch.bfloat16, 4, q)
+    if out.shape != q.shape:
+        raise ValueError("out must be shaped like q")
+    return out
+
+
+def _own_workspace(workspace, size, q):
+    """(pointer, bytes) of the workspace given, or of a new one of size() bytes."""
+    if workspace is None:
+        n = size()
+        if n == 0:
+            return None, 0, None
+        workspace = _torch().empty(n, dtype=_torch().uint8, device=q.device)
+    _check_workspace(workspace, q)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def make_blocks_workspace(q, k, topk: int, block_size: int = 64):
+    """A workspace for attention_blocks on these shapes (None where none is needed)."""
+    B, Hq, Sq, D = q.shape
+    n = int(ef_attention_blocks_workspace_size(B, Hq, k.shape[1], Sq, k.shape[2], D, block_size,
+                                               topk))
+    return _torch().empty(n, dtype=_torch().uint8, device=q.device) if n else None
+
+
+def attention_blocks(q, k, v, blocks, block_size: int = 64, scale: Optional[float] = None,
+                     lengths=None, workspace=None, out=None, stream=None):
+    """Attention of each query over the keys up to its own in its listed blocks, through
+    ef_attention_blocks; blocks is int32 [B, Hkv, Sq, topk] (see block_select). Returns bf16
+    shaped like q."""
+    torch = _torch()
+    B, Hq, Hkv, Sq, Skv, D = _check_qkv(q, k, v)
+    for name, t in (("k", k), ("v", v)):
+        _same_device(t, q, name)
+    _check_tensor(blocks, "blocks", torch.int32, 4, q)
+    topk = blocks.shape[3]
+    if blocks.shape[:3] != (B, Hkv, Sq):
+        raise ValueError(f"blocks must be [{B}, {Hkv}, {Sq}, topk], got {tuple(blocks.shape)}")
+    if scale is None:
+        scale = 1.0 / math.sqrt(D)
+    o = _out_bf16(q, out)
+    ptr, n, workspace = _own_workspace(
+        workspace, lambda: ef_attention_blocks_workspace_size(B, Hq, Hkv, Sq, Skv, D, block_size,
+                                                              topk), q)
+    st = _call_on(q, stream, ef_attention_blocks, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                  blocks.data_ptr(), _lengths_ptr(lengths, B, q), o.data_ptr(), B, Hq, Hkv, Sq,
+                  Skv, D, float(scale), block_size, topk, ptr, n)
+    _check(st, "ef_attention_blocks")
+    return o
+
+
+def make_shared_prefix_workspace(q, k_prefix, k):
+    """A workspace for attention_shared_prefix on these shapes (None where none is needed)."""
+    B, Hq, Sq, D = q.shape
+    n = int(ef_attention_shared_prefix_workspace_size(B, Hq, k.shape[1], Sq, k_prefix.shape[1],
+                                                      k.shape[2], D))
+    return _torch().empty(n, dtype=_torch().uint8, device=q.device) if n else None
+
+
+def attention_shared_prefix(q, k_prefix, v_prefix, k, v, scale: Optional[float] = None,
+                            causal: bool = True, lengths=None, workspace=None, out=None,
+                            stream=None):
+    """Attention of every sequence over the prefix k_prefix, v_prefix [Hkv, Lp, D] and then its
+    own keys k, v [B, Hkv, Skv, D], through ef_attention_shared_prefix. Returns bf16 shaped like
+    q."""
+    torch = _torch()
+    B, Hq, Hkv, Sq, Skv, D = _check_qkv(q, k, v)
+    for name, t in (("k", k), ("v", v)):
+        _same_device(t, q, name)
+    _check_tensor(k_prefix, "k_prefix", torch.bfloat16, 3, q)
+    _check_tensor(v_prefix, "v_prefix", torch.bfloat16, 3, q)
+    Lp = k_prefix.shape[1]
+    if k_prefix.shape != (Hkv, Lp, D) or v_prefix.shape != k_prefix.shape:
+        raise ValueError("k_prefix and v_prefix must be [Hkv, Lp, D] matching k")
+    if scale is None:
+        scale = 1.0 / math.sqrt(D)
+    o = _out_bf16(q, out)
+    ptr, n, workspace = _own_workspace(
+        workspace, lambda: ef_attention_shared_prefix_workspace_size(B, Hq, Hkv, Sq, Lp, Skv, D),
+        q)
+    st = _call_on(q, stream, ef_attention_shared_prefix, q.data_ptr(), k_prefix.data_ptr(),
+                  v_prefix.data_ptr(), k.data_ptr(), v.data_ptr(), _lengths_ptr(lengths, B, q),
+                  o.data_ptr(), B, Hq, Hkv, Sq, Lp, Skv, D, float(scale), causal, ptr, n)
+    _check(st, "ef_attention_shared_prefix")
+    return o

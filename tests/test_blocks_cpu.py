@@ -32,14 +32,39 @@ def select(**kw):
                               a["Skv"], a["D"], a["bs"], a["K"], a["sinks"], a["local"], None)
 
 
+def blocks(**kw):
+    a = dict(q=A, k=A, v=A, x=A, n=None, o=A, B=1, Hq=4, Hkv=2, Sq=3, Skv=1000, D=128, scale=0.1,
+             bs=64, K=8, ws=A, wsb=1 << 40)
+    a.update(kw)
+    return ef.ef_attention_blocks(a["q"], a["k"], a["v"], a["x"], a["n"], a["o"], a["B"], a["Hq"],
+                                  a["Hkv"], a["Sq"], a["Skv"], a["D"], a["scale"], a["bs"],
+                                  a["K"], a["ws"], a["wsb"], None)
+
+
+def prefix(**kw):
+    a = dict(q=A, kp=A, vp=A, k=A, v=A, n=None, o=A, B=2, Hq=4, Hkv=2, Sq=3, Lp=500, Skv=1000,
+             D=128, scale=0.1, causal=1, ws=A, wsb=1 << 40)
+    a.update(kw)
+    return ef.ef_attention_shared_prefix(a["q"], a["kp"], a["vp"], a["k"], a["v"], a["n"], a["o"],
+                                         a["B"], a["Hq"], a["Hkv"], a["Sq"], a["Lp"], a["Skv"],
+                                         a["D"], a["scale"], a["causal"], a["ws"], a["wsb"], None)
+
+
 @needs_lib
-@pytest.mark.parametrize("call", [summary, select], ids=["summary", "select"])
+@pytest.mark.parametrize("call", [summary, select, blocks, prefix],
+                         ids=["summary", "select", "blocks", "prefix"])
 def test_refusals(call):
     assert call(D=96) == 4
     assert call(B=-1) == 2
     assert call(Hkv=0) == 2
     assert call(Skv=-1) == 2
     assert call(B=70000) == 2
+    assert call(Skv=2**24, D=128) == 2
+
+
+@needs_lib
+@pytest.mark.parametrize("call", [summary, select, blocks], ids=["summary", "select", "blocks"])
+def test_refused_blocks(call):
     assert call(bs=32) == 14
     assert call(bs=0) == 14
     assert call(bs=-64) == 14
@@ -72,6 +97,62 @@ def test_refusals_of_their_own():
     assert select(sinks=2**31 - 1, local=2**31 - 1) == 14
     assert select(Sq=0, q=None, o=None) == 0
     assert ef.library().ef_status_string(14) != b"unknown status"
+
+
+@needs_lib
+@pytest.mark.parametrize("call", [blocks, prefix], ids=["blocks", "prefix"])
+def test_refused_attention(call):
+    assert call(Hq=5) == 3
+    assert call(Hq=0) == 2
+    assert call(Sq=-1) == 2
+    assert call(Sq=2**24) == 2
+    # Rows of the whole batch are counted in 32 bits.
+    assert call(B=512, Hq=64, Hkv=64, Sq=2**16) == 2
+    for name in ("q", "k", "v", "o"):
+        assert call(**{name: None}) == 1
+        assert call(**{name: MIS}) == 5
+    assert call(scale=float("nan")) == 8
+    assert call(scale=float("inf")) == 8
+    assert call(ws=None) == 7
+    assert call(wsb=100) == 7
+    assert call(ws=MIS) == 5
+    assert call(B=0, q=None, k=None, v=None, o=None, ws=None) == 0
+    assert call(Sq=0, q=None, k=None, v=None, o=None, ws=None) == 0
+
+
+@needs_lib
+def test_refused_lists_and_prefixes():
+    assert blocks(x=None) == 1
+    assert blocks(x=MIS) == 5
+    assert blocks(K=0) == 14
+    assert blocks(K=257) == 14
+    assert prefix(Lp=-1) == 2
+    assert prefix(Lp=2**24) == 2
+    assert prefix(kp=None) == 1
+    assert prefix(vp=None) == 1
+    assert prefix(kp=MIS) == 5
+    assert prefix(vp=MIS) == 5
+
+
+@needs_lib
+def test_workspace_sizes():
+    size = ef.ef_attention_blocks_workspace_size
+    assert size(1, 4, 2, 3, 1000, 96, 64, 8) == 0
+    assert size(1, 4, 2, 3, 1000, 128, 65, 8) == 0
+    assert size(1, 4, 2, 3, 1000, 128, 64, 0) == 0
+    assert size(0, 4, 2, 3, 1000, 128, 64, 8) == 0
+    assert size(1, 4, 2, 1, 1000, 128, 64, 1) == 0     # one block: nothing to share
+    assert size(1, 32, 8, 4096, 8192, 128, 64, 16) == 0  # row tiles fill the chip
+    n = size(1, 32, 8, 1, 16384, 128, 64, 16)
+    assert n > 0
+    assert blocks(B=1, Hq=32, Hkv=8, Sq=1, Skv=16384, K=16, wsb=n - 1) == 7
+    size = ef.ef_attention_shared_prefix_workspace_size
+    assert size(2, 4, 2, 3, 500, 1000, 96) == 0
+    assert size(2, 4, 2, 3, -1, 1000, 128) == 0
+    assert size(2, 4, 2, 3, 0, 0, 128) == 0
+    n = size(2, 4, 2, 3, 500, 1000, 128)
+    assert n > 0
+    assert prefix(wsb=n - 1) == 7
 
 
 def test_oracle_summary_and_selection():

@@ -3,47 +3,19 @@ fp64 oracle.
 
 Tolerances. A summary is an fp32 sum rounded to bf16 once: half a step of the value (2^-8) plus
 one rounding (2^-24) of a partial sum per key, each at most the sum of the keys' magnitudes. A
-selection is compared for equality. The tolerance of the attention is derived at its test.
+selection is compared for equality. The tolerance of the
+attention is derived in long_helpers.py.
 """
-
-import os
-import sys
 
 import numpy as np
 import pytest
 import torch
 
 import oracle
+from long_helpers import _gpu, announce, close, f64, lengths_of, normal, poison  # noqa: F401
 from paper_2609_12330_amd import ef_attention as ef
 
 pytestmark = pytest.mark.gpu
-
-
-def announce(msg):
-    print(f"[gpu case] {msg}", file=sys.stderr, flush=True)
-
-
-@pytest.fixture(scope="module", autouse=True)
-def _gpu():
-    if not torch.cuda.is_available():
-        pytest.skip("no GPU")
-    if not os.path.exists(ef.LIB_PATH):
-        raise RuntimeError("libef_attention.so is not built; the HIP path must be present")
-    ef.library()
-    yield
-
-
-def f64(t):
-    return t.double().cpu().numpy()
-
-
-def normal(seed, *shape):
-    g = torch.Generator("cpu").manual_seed(seed)
-    return torch.randn(shape, generator=g).to(torch.bfloat16)
-
-
-def lengths_of(values):
-    return None if values is None else torch.tensor(values, dtype=torch.int32, device="cuda")
 
 
 def same_lists(got, ref):
@@ -190,3 +162,105 @@ def test_select_degenerate(what):
     with np.errstate(invalid="ignore"):
         ref = oracle.block_select_ref(f64(q), f64(m), S, K, bs, 1, 1)
     same_lists(got, ref)
+
+
+# ------------------------------------------------------------------------------- attention
+
+
+def random_lists(seed, B, H, Sq, K, nb, junk=False):
+    """Distinct blocks of [0, nb) in random order; with junk also repeats, -1 and blocks that do
+    not exist."""
+    g = torch.Generator("cpu").manual_seed(seed)
+    x = torch.rand(B, H, Sq, max(nb, K), generator=g).argsort(-1)[..., :K].to(torch.int32)
+    x = torch.where(x < nb, x, -1)
+    if junk and K > 3:
+        x[..., 1] = x[..., 0]
+        x[..., 2] = nb + 5
+        x[..., 3] = -7
+    return x.contiguous()
+
+
+# (B, Hq, Hkv, Sq, Skv, D, block, topk, lengths, junk)
+ATTENTION = [
+    (1, 1, 1, 1, 1, 64, 64, 1, None, False),
+    (1, 4, 1, 1, 63, 128, 64, 3, None, False),
+    (2, 8, 2, 1, 1000, 128, 64, 5, [1000, 65], False),
+    (3, 8, 2, 1, 2000, 64, 128, 7, [2000, 0, 129], True),
+    (2, 4, 4, 7, 900, 128, 64, 4, [900, 3], True),     # queries before the first key
+    (1, 12, 4, 50, 1200, 128, 64, 6, None, False),     # groups of 3: tiles cut positions
+    (1, 12, 2, 40, 777, 64, 128, 3, None, True),       # groups of 6
+    (2, 6, 6, 130, 1500, 64, 64, 8, [1500, 200], False),  # 64 positions to a tile
+    (1, 8, 2, 200, 200, 128, 64, 2, None, False),
+    (1, 64, 1, 3, 1111, 128, 64, 9, None, False),      # groups of 64
+    (1, 2, 2, 64, 64 * 700, 64, 64, 16, None, False),  # a union of more than one window
+    (1, 2, 2, 3, 64 * 1500, 64, 64, 250, None, False),  # ... and split over workgroups
+    (1, 4, 4, 150, 128 * 300, 128, 128, 12, None, True),
+]
+
+
+def attend_blocks(shape, seed=20, scale=None, lists=None):
+    B, Hq, H, Sq, S, D, bs, K, n, junk = shape
+    q, k, v = normal(seed, B, Hq, Sq, D), normal(seed + 1, B, H, S, D), normal(seed + 2, B, H, S, D)
+    if lists is None:
+        lists = random_lists(seed + 3, B, H, Sq, K, -(-S // bs), junk)
+    scale = D ** -0.5 if scale is None else scale
+    got = ef.attention_blocks(q.cuda(), poison(k, n), poison(v, n), lists.cuda(), bs, scale=scale,
+                              lengths=lengths_of(n))
+    torch.cuda.synchronize()
+    args = (f64(q), f64(k), f64(v))
+    ref = oracle.attention_blocks_ref(*args, lists.numpy(), bs, scale, n)
+    mag = oracle.attention_blocks_ref(*args[:2], np.abs(args[2]), lists.numpy(), bs, scale, n)
+    close(got, ref, mag, shape)
+    return got, ref
+
+
+@pytest.mark.parametrize("shape", ATTENTION, ids=str)
+def test_attention_blocks(shape):
+    announce(f"attention_blocks {shape}")
+    attend_blocks(shape)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1.0])
+def test_attention_blocks_scale(scale):
+    announce(f"attention_blocks scale {scale}")
+    # A scale of 1 makes scores of up to 11 sqrt(128) = 128: their error grows with it, and the
+    # weights' with them by e^(1.5e-5 * 1.6 * 128) - 1 = 3e-3: the tolerance's 1e-3 is too small
+    # for D = 128, so D = 64 and short keys (|q| |k| of about 64 / 4).
+    B, Hq, H, Sq, S, D = 1, 8, 2, 20, 700, 64
+    q, k, v = normal(30, B, Hq, Sq, D), normal(31, B, H, S, D) / 4, normal(32, B, H, S, D)
+    lists = random_lists(33, B, H, Sq, 6, 11)
+    got = ef.attention_blocks(q.cuda(), k.cuda(), v.cuda(), lists.cuda(), 64, scale=scale)
+    torch.cuda.synchronize()
+    args = (f64(q), f64(k))
+    ref = oracle.attention_blocks_ref(*args, f64(v), lists.numpy(), 64, scale)
+    mag = oracle.attention_blocks_ref(*args, np.abs(f64(v)), lists.numpy(), 64, scale)
+    close(got, ref, mag, scale)
+
+
+def test_attention_blocks_without_blocks():
+    """Empty lists, and lists of blocks behind the query only, give zero rows."""
+    announce("attention_blocks empty lists")
+    B, Hq, H, Sq, S, D, K = 2, 4, 2, 9, 640, 128, 4
+    q, k = normal(34, B, Hq, Sq, D).cuda(), normal(35, B, H, S, D).cuda()
+    lists = torch.full((B, H, Sq, K), -1, dtype=torch.int32, device="cuda")
+    lists[0] = 9  # keys 576 .. 639: of sequence 0 only the last query sees one, key 576
+    n = torch.tensor([577, 640], dtype=torch.int32, device="cuda")
+    out = torch.full_like(q, 3.0)
+    ef.attention_blocks(q, k, k, lists, lengths=n, out=out)
+    torch.cuda.synchronize()
+    assert (out[0, :, :-1] == 0).all() and (out[1] == 0).all()
+    assert torch.equal(out[0, :, -1], k[0, :, 576].repeat_interleave(Hq // H, 0))
+
+
+def test_all_blocks_is_plain_causal_attention():
+    announce("attention_blocks against attention_fwd")
+    B, Hq, H, Sq, S, D = 1, 8, 2, 300, 1500, 128
+    q, k, v = (normal(40 + i, B, h, n, D).cuda() for i, (h, n) in
+               enumerate(((Hq, Sq), (H, S), (H, S))))
+    every = torch.arange(24, dtype=torch.int32, device="cuda").expand(B, H, Sq, 24).contiguous()
+    got = ef.attention_blocks(q, k, v, every)
+    ref = ef.attention_fwd(q, k, v, causal=True)
+    mag = ef.attention_fwd(q, k, v.abs(), causal=True)
+    torch.cuda.synchronize()
+    # Both round the weights: twice the tolerance of one.
+    close(got, f64(ref), 2 * f64(mag), "plain")
