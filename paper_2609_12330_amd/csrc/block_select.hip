@@ -5,26 +5,41 @@
 // s_n the block's summary, ties to the lower index. The result is the one that
 // exact arithmetic gives, in ascending order, filled with -1.
 //
-// Scores: a 16x16x32 bf16 product, 16 summaries (A) times 16 columns of queries
-// (B). A position's heads take adjacent columns, padded to a power of two by
-// repeating the last head, so the maximum over them is a few DPP moves. A
-// workgroup scores `pos` positions against all blocks they may choose from and
-// keeps the scores in LDS; each wave then chooses for its own positions.
+// Scores: a 16x16x32 bf16 product, 16 rows of queries (A) times 16 summaries (B). A
+// position's heads take adjacent rows, padded to a power of two by repeating the last
+// head: a lane holds four rows of a block, so the maximum over the heads is taken in
+// registers. A workgroup scores `pos` positions against all blocks they may choose
+// from and keeps the scores in LDS; each wave then chooses for its own positions.
 //
-// Choice: the need-th largest score is found by bisection over the bits of the
-// scores (as order-preserving integers), counting with ballots. fp32 products
-// differ from exact ones by at most E = 2 D 2^-24 max|q| max|s| (2-norms; every
-// one of the D additions rounds, or truncates, once; bf16 products are exact), so
-// where the last score in and the first one out are more than 2 E apart the choice
-// is the exact one. Elsewhere only the blocks within 2 E of the border are scored
-// again in 64 bits (products of bf16 are exact there and their sum is to 2^-53),
-// in index order, and the best of them complete the list.
+// Choice: fp32 products differ from exact ones by at most E = 2 D 2^-24 max|q| max|s|
+// (2-norms; every one of the D additions rounds, or truncates, once; bf16 products are
+// exact), so where the last score in and the first one out are more than 2 E apart the
+// choice by fp32 scores is the exact one. Elsewhere only the blocks within 2 E of the
+// border are scored again in 64 bits (products of bf16 are exact there and their sum
+// is to 2^-53), in index order, and the best of them complete the list.
+//
+// The need-th largest of the scores, every 64th in a lane's registers, is bounded from
+// below by the need-th largest of the lanes' largest ones, which a bisection between
+// their smallest and largest finds, each step one ballot (a somewhat lower bound does,
+// so it stops early). The few scores above that bound less 2 E then go one to a lane,
+// in index order, for a second bisection. They hold every block within 2 E of the
+// border too. Where that does not apply (need > 64, or more than 64
+// such scores, as where many are equal) a bisection over order-preserving integers counts all
+// scores, and a border of any length is settled in LDS.
 #include "ef_long.hpp"
 #include "ef_device.hpp"
+
+#include <type_traits>
 
 namespace ef {
 
 namespace {
+
+// LDS pointers by type: through plain ones the compiler loses sight of the address space
+// and reads LDS with flat loads, which wait for each other (choice of a position 5.6
+// -> ?).
+typedef __attribute__((address_space(3))) float lds_float;
+typedef __attribute__((address_space(3))) unsigned long long lds_u64;
 
 // Order-preserving integer of a float (no NaN).
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -32,12 +47,33 @@ __device__ __forceinline__ uint32_t ordered(float x) {
   return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
 }
 
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) x = fmaxf(x, shfl_xor(x, m));
-  return x;
+__device__ __forceinline__ float unordered(uint32_t u) {
+  return __uint_as_float(u ^ ((u >> 31) ? 0x80000000u : 0xffffffffu));
 }
-__device__ __forceinline__ float wave_min(float x) { return -wave_max(-x); }
+
+// Reductions over the wave's lanes, in DPP moves and lane swaps.
+template <class T, class F>
+__device__ __forceinline__ T wave_reduce(T x, F f) {
+  static_assert(sizeof(T) == 4, "a lane register");
+  auto bits = [](T v) { return __builtin_bit_cast(float, v); };
+  auto val = [](float v) { return __builtin_bit_cast(T, v); };
+  x = f(x, val(dpp_mov<kDppQuadXor1>(bits(x))));
+  x = f(x, val(dpp_mov<kDppQuadXor2>(bits(x))));
+  x = f(x, val(dpp_mov<kDppHalfMirror>(bits(x))));
+  x = f(x, val(dpp_mov<kDppRowRor8>(bits(x))));
+  float a, b;
+  lane_pair<16>(bits(x), a, b);
+  x = f(val(a), val(b));
+  lane_pair<32>(bits(x), a, b);
+  return f(val(a), val(b));
+}
+__device__ __forceinline__ float wave_max(float x) {
+  return wave_reduce(x, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  return wave_reduce(x, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+__device__ __forceinline__ uint32_t wave_min(uint32_t x) { return ~wave_max(~x); }
 
 // LDS written by other lanes of this wave becomes visible to it.
 __device__ __forceinline__ void wave_lds_sync() {
@@ -45,31 +81,61 @@ __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// score(n) in 64 bits, by one wave; NaN counts as -inf.
+// f applied to x and the same value of other lanes: those at a DPP move's distance, or
+// (OFF = 16, 32) lane l ^ OFF.
+template <int CTRL>
+__device__ __forceinline__ double dpp_mov64(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const float lo = dpp_mov<CTRL>(__uint_as_float((uint32_t)u));
+  const float hi = dpp_mov<CTRL>(__uint_as_float((uint32_t)(u >> 32)));
+  return __builtin_bit_cast(double, (uint64_t)__float_as_uint(hi) << 32 | __float_as_uint(lo));
+}
+template <int OFF>
+__device__ __forceinline__ double pair_max64(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  float l0, l1, h0, h1;
+  lane_pair<OFF>(__uint_as_float((uint32_t)u), l0, l1);
+  lane_pair<OFF>(__uint_as_float((uint32_t)(u >> 32)), h0, h1);
+  auto join = [](float lo, float hi) {
+    return __builtin_bit_cast(double, (uint64_t)__float_as_uint(hi) << 32 | __float_as_uint(lo));
+  };
+  const double p = join(l0, h0), q = join(l1, h1);
+  return p > q ? p : q;
+}
+
+// score(n) in 64 bits, by one wave, the same in every lane; NaN counts as -inf. 16
+// lanes take a head, four heads at a time.
 template <int D>
-__device__ double exact_score(const uint16_t* q, size_t head_stride, int G, const uint16_t* s) {
-  constexpr int E = D / 64;  // elements per lane
+__device__ __forceinline__ double exact_score(const uint16_t* q, size_t head_stride, int G, const uint16_t* s) {
+  constexpr int W = D / 32;  // words of two elements per lane
   const int lane = threadIdx.x & 63;
-  double best = -__builtin_inf();
-  double m[E];
+  const int sub = lane & 15;
+  uint32_t sw[W];
 #pragma unroll
-  for (int e = 0; e < E; ++e) m[e] = (double)__uint_as_float((uint32_t)s[lane + 64 * e] << 16);
-  for (int g = 0; g < G; ++g) {
-    const uint16_t* qg = q + g * head_stride;
+  for (int e = 0; e < W; ++e) sw[e] = reinterpret_cast<const uint32_t*>(s)[sub * W + e];
+  double best = -__builtin_inf();
+  for (int g = lane >> 4; g - (lane >> 4) < G; g += 4) {
+    const uint32_t* qg =
+        reinterpret_cast<const uint32_t*>(q + min(g, G - 1) * head_stride) + sub * W;
     double x = 0.0;
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      x += m[e] * (double)__uint_as_float((uint32_t)qg[lane + 64 * e] << 16);
-#pragma unroll
-    for (int off = 1; off < 64; off *= 2) x += __shfl_xor(x, off, 64);
+    for (int e = 0; e < W; ++e) {
+      const uint32_t w = qg[e];
+      x += (double)bf16lo_to_f32(sw[e]) * (double)bf16lo_to_f32(w);
+      x += (double)bf16hi_to_f32(sw[e]) * (double)bf16hi_to_f32(w);
+    }
+    x += dpp_mov64<kDppQuadXor1>(x);
+    x += dpp_mov64<kDppQuadXor2>(x);
+    x += dpp_mov64<kDppHalfMirror>(x);
+    x += dpp_mov64<kDppRowRor8>(x);
     if (x > best) best = x;  // false for NaN
   }
-  return best;
+  return pair_max64<32>(pair_max64<16>(best));
 }
 
 // Whether the queries of all G heads of a position are 0.
 template <int D>
-__device__ bool all_zero(const uint16_t* q, size_t head_stride, int G) {
+__device__ __forceinline__ bool all_zero(const uint16_t* q, size_t head_stride, int G) {
   const int lane = threadIdx.x & 63;
   uint32_t x = 0;
   for (int g = 0; g < G; ++g)
@@ -82,7 +148,7 @@ __device__ bool all_zero(const uint16_t* q, size_t head_stride, int G) {
 // [lo, hi], by exact score: their scores become +inf, the others' -inf. The best
 // so far are held by the lanes, entry i in slot i / 64 of lane i % 64.
 template <int D>
-__device__ void settle_border(float* sc, int c0, int c1, float lo, float hi, int want,
+__device__ __forceinline__ void settle_border(lds_float* sc, int c0, int c1, float lo, float hi, int want,
                               const uint16_t* q, size_t head_stride, int G, const uint16_t* s) {
   constexpr int SLOTS = kMaxTopk / 64;
   const int lane = threadIdx.x & 63;
@@ -101,9 +167,8 @@ __device__ void settle_border(float* sc, int c0, int c1, float lo, float hi, int
     unsigned long long todo = __ballot(in);
     if (in) sc[n] = kNegInf;
     while (todo) {
-      const int j = __builtin_ctzll(todo);
+      const int m = base + __builtin_ctzll(todo);
       todo &= todo - 1;
-      const int m = base + j;
       const double e = exact_score<D>(q, head_stride, G, s + (size_t)m * D);
       int at = held;  // entry that takes the block, -1: none
       if (held == want) {
@@ -146,110 +211,388 @@ __device__ void settle_border(float* sc, int c0, int c1, float lo, float hi, int
   wave_lds_sync();
 }
 
-// CT: 16-column tiles of queries per workgroup (G <= 16); 1 with `per` passes
-// for G > 16.
-template <int D, int CT, int NW>
-__global__ __launch_bounds__(NW * 64) void block_select_kernel(SelectParams a) {
+// The scores of the blocks [c0, c1) of one position as integers, every 64th in a
+// lane's registers; with NV = 0 (more than 64 a lane) they stay in LDS.
+template <int NV>
+struct Keys {
+  const lds_float* sc;
+  int c0, c1;
+  uint32_t u[NV > 0 ? NV : 1];
+  __device__ __forceinline__ uint32_t fetch(int i) const {  // 0: no block; NaN is -inf
+    const int n = c0 + 64 * i + (threadIdx.x & 63);
+    const float x = sc[min(n, c1 - 1)];
+    return n < c1 ? ordered(x == x ? x : kNegInf) : 0u;
+  }
+  __device__ __forceinline__ void load() {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) u[i] = fetch(i);
+  }
+  // f(i, key of block c0 + 64 i + lane), ascending in i, all lanes together.
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) f(i, u[i]);
+    } else {
+      for (int i = 0; c0 + 64 * i < c1; ++i) f(i, fetch(i));
+    }
+  }
+  __device__ __forceinline__ int count(uint32_t least) const {
+    int k = 0;
+    each([&](int, uint32_t x) { k += (int)__popcll(__ballot(x >= least)); });
+    return k;
+  }
+};
+
+// One position's choice among the blocks [c0, c1), which are more than the `need` wanted
+// ones, by one wave. sc: the scores (NaN where every head's product was); bound: their
+// largest error.
+struct Choice {
+  lds_float* sc;
+  int c0, c1, need;
+  float bound;
+  bool summaries;  // whether some summary is not 0
+  const uint16_t* q;  // the position's first head
+  size_t head_stride;
+  int G;
+  const uint16_t* s;  // summaries of the kv head
+  int* out;           // the position's list from its entry c0 on
+
+  // Scores closer than this may change places (a score of -inf adds nothing to it; an
+  // infinite bound stays infinite).
+  __device__ __forceinline__ float apart(float x) const {
+    return 2.f * bound + (fabsf(x) < -kNegInf ? 4.8e-7f * fabsf(x) : 0.f) + 1e-30f;
+  }
+};
+
+// The choice where few scores come into question; false, with nothing written, where
+// they are not few. scratch: 65 words of LDS.
+template <int D, int NV>
+__device__ __forceinline__ bool choose_few(const Choice& a, lds_u64* scratch) {
+  const int lane = threadIdx.x & 63;
+  const int c0 = a.c0, c1 = a.c1, need = a.need;
+  Keys<NV> keys{a.sc, c0, c1, {}};
+  keys.load();
+  uint32_t mine = 0;  // this lane's largest
+  keys.each([&](int, uint32_t x) { mine = max(mine, x); });
+  const uint32_t top = __builtin_amdgcn_readfirstlane(wave_max(mine));
+  // The few scores that can be in or near the border, one to a lane, in index order.
+  uint32_t few = 0;
+  int few_block = 0, held = c1 - c0;
+  if (held <= 64) {
+    few = keys.fetch(0);
+    few_block = c0 + lane;
+  } else if (need <= 64) {
+    // Halving the interval of values takes a step per bit of the answer's place among
+    // them; the integers' would first look for its exponent.
+    const float best = unordered(mine);
+    float least = unordered(__builtin_amdgcn_readfirstlane(wave_min(mine)));
+    float hi = unordered(top);
+    for (int k = 64, most = need + (64 - need) / 4, step = 0; k > most && step < 16; ++step) {
+      const float mid = 0.5f * least + 0.5f * hi;
+      const int n = (int)__popcll(__ballot(best >= mid));
+      if (n >= need && mid > least) {
+        least = mid;
+        k = n;
+      } else {
+        hi = mid;  // (NaN with infinite ends: no further step changes anything)
+      }
+    }
+    const float margin = fmaxf(a.apart(least), a.apart(unordered(top)));
+    const uint32_t base = margin < -kNegInf && least > kNegInf ? ordered(least - margin) : 0u;
+    held = 0;
+    keys.each([&](int i, uint32_t x) {
+      const unsigned long long m = __ballot(x >= base);
+      const int slot = held + (int)__builtin_amdgcn_mbcnt_hi(
+                                  (uint32_t)(m >> 32),
+                                  __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
+      // Word 64 takes what has no place.
+      scratch[x >= base ? min(slot, 64) : 64] =
+          (unsigned long long)x << 32 | (uint32_t)(c0 + 64 * i + lane);
+      held += (int)__popcll(m);
+    });
+    if (held <= 64) {
+      wave_lds_sync();
+      const unsigned long long w = scratch[lane];
+      if (lane < held) {
+        few = (uint32_t)(w >> 32);
+        few_block = (int)(uint32_t)w;
+      }
+    }
+    wave_lds_sync();  // read before the wave's next position writes
+  }
+  if (held <= 64) {
+    // A T with just `need` of the few at or above it, or the largest with at least that
+    // many: by halves of the interval of values, then of the integers between.
+    uint32_t T = __builtin_amdgcn_readfirstlane(wave_min(lane < held ? few : 0xffffffffu));
+    uint32_t hi = top;
+    int cnt = held;
+    for (int step = 0; cnt != need && T < hi; ++step) {
+      uint32_t mid = ordered(0.5f * unordered(T) + 0.5f * unordered(hi));
+      if (step >= 16 || mid <= T || mid > hi) mid = hi - (hi - T) / 2;
+      const int n = (int)__popcll(__ballot(few >= mid));
+      if (n >= need) {
+        T = mid;
+        cnt = n;
+      } else {
+        hi = mid - 1;
+      }
+    }
+    bool take = few >= T;
+    // Last score in, first one out (where that is none of the few, more than e2 below).
+    const float least = unordered(wave_min(take ? few : 0xffffffffu));
+    const uint32_t second = wave_max(take ? 0u : few);
+    const float e2 = a.apart(least);
+    if (__builtin_expect(
+            cnt != need || (second != 0 && !(least - unordered(second) > e2)), 0)) {
+      const float x = unordered(few);
+      const bool finite = e2 < -kNegInf && least > kNegInf;
+      const bool sure = few != 0 && finite && x > least + e2;
+      const bool near = few != 0 && !sure && (!finite || x >= least - e2);
+      const unsigned long long todo = __ballot(near);
+      const int want = need - (int)__popcll(__ballot(sure));
+      double exact = 0.0;
+      for (unsigned long long m = todo; m; m &= m - 1) {
+        const int j = __builtin_ctzll(m);
+        const int n = __builtin_amdgcn_readlane(few_block, j);
+        const double e = exact_score<D>(a.q, a.head_stride, a.G, a.s + (size_t)n * D);
+        if (lane == j) exact = e;
+      }
+      int rank = 0;  // blocks near the border that come before this lane's
+      for (unsigned long long m = todo; m; m &= m - 1) {
+        const int j = __builtin_ctzll(m);
+        const double e = __shfl(exact, j, 64);
+        rank += e > exact || (e == exact && j < lane) ? 1 : 0;
+      }
+      take = sure || (near && rank < want);
+    }
+    const int slot = (int)__popcll(__ballot(take) & ((1ull << lane) - 1));
+    if (take && slot < need) a.out[slot] = few_block;
+    return true;
+  }
+  return false;
+}
+
+// The choice where many scores are equal or many blocks wanted.
+template <int D>
+__device__ __forceinline__ void choose_many(const Choice& a) {
+  const int lane = threadIdx.x & 63;
+  const int c0 = a.c0, c1 = a.c1, need = a.need;
+  lds_float* const sc = a.sc;
+  const Keys<0> keys{sc, c0, c1, {}};
+  uint32_t top = 0;
+  keys.each([&](int, uint32_t x) { top = max(top, x); });
+  top = __builtin_amdgcn_readfirstlane(wave_max(top));
+  int cnt = c1 - c0;
+  uint32_t T = 0;
+  for (uint32_t hi = top; cnt != need && T < hi;) {
+    const uint32_t mid = hi - (hi - T) / 2;
+    const int n = keys.count(mid);
+    if (n >= need) {
+      T = mid;
+      cnt = n;
+    } else {
+      hi = mid - 1;
+    }
+  }
+  uint32_t in = 0xffffffffu, outside = 0;
+  keys.each([&](int, uint32_t x) {
+    in = min(in, x >= T ? x : 0xffffffffu);
+    outside = max(outside, x >= T ? 0u : x);
+  });
+  const float least = unordered(wave_min(in));
+  const float next = cnt != need ? least : unordered(wave_max(outside));
+  const float e2 = a.apart(least);
+  if (!(least - next > e2)) {
+    for (int n = c0 + lane; n < c1; n += 64)
+      if (sc[n] != sc[n]) sc[n] = kNegInf;
+    wave_lds_sync();
+    // Scores that are -inf (NaN), or 0 because all summaries or all of the
+    // position's queries are, need no second look: their indices decide.
+    const bool finite = e2 < -kNegInf;
+    const bool settled =
+        (finite && least == kNegInf) || !a.summaries || all_zero<D>(a.q, a.head_stride, a.G);
+    const float lo = settled ? least : finite ? least - e2 : kNegInf;
+    const float hi = settled ? least : finite ? least + e2 : -kNegInf;
+    int sure = 0;
+    for (int base = c0; base < c1; base += 64) {
+      const int n = base + lane;
+      sure += (int)__popcll(__ballot(n < c1 && sc[min(n, c1 - 1)] > hi));
+    }
+    int want = need - sure;
+    float thr = hi;
+    if (settled) {
+      for (int base = c0; base < c1; base += 64) {
+        const int n = base + lane;
+        const bool tie = n < c1 && sc[min(n, c1 - 1)] == least;
+        const unsigned long long m = __ballot(tie);
+        const int rank = (int)__popcll(m & ((1ull << lane) - 1));
+        if (tie) sc[n] = rank < want ? -kNegInf : kNegInf;
+        want = max(want - (int)__popcll(m), 0);
+      }
+      wave_lds_sync();
+      thr = least == kNegInf ? -3.402823466e+38f : least;
+    } else {
+      settle_border<D>(sc, c0, c1, lo, hi, want, a.q, a.head_stride, a.G, a.s);
+    }
+    T = ordered(thr);
+  }
+  int at = 0;
+  keys.each([&](int i, uint32_t x) {
+    const bool take = x >= T;
+    const unsigned long long m = __ballot(take);
+    const int slot = at + (int)__popcll(m & ((1ull << lane) - 1));
+    if (take && slot < need) a.out[slot] = c0 + 64 * i + lane;
+    at += (int)__popcll(m);
+  });
+}
+
+// CT: 16-row tiles of queries per workgroup (G <= 16); 1 with `per` passes for
+// G > 16. AHEAD: tiles of summaries a wave requests at once. LDS: floats of the score
+// rows, 0: given at launch.
+template <int D, int CT, int NW, int AHEAD, int LDS>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
+void block_select_kernel(SelectParams a) {
   constexpr int KS = D / 32;  // k-steps of the product
-  extern __shared__ __align__(16) float scores[];  // [pos][stride]
+  extern __shared__ __align__(16) float launch_lds[];
+  __shared__ __align__(16) float fixed_lds[LDS > 0 ? LDS : 4];
+  float* const scores = LDS > 0 ? fixed_lds : launch_lds;  // [pos][stride]
+  __shared__ unsigned long long scratch[NW][66];
   __shared__ float norms[NW];
   __shared__ uint32_t nonzero[NW];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int bh = blockIdx.x / a.ptiles, pt = blockIdx.x % a.ptiles;
   const int b = bh / a.Hkv, hkv = bh % a.Hkv;
-  const int len = sequence_length(a.lengths, b, a.Skv);
   const int p0 = pt * a.pos, npos = min(a.pos, a.Sq - p0);
+  const uint16_t* sh = a.s + (size_t)bh * a.NB * D;
+  const uint16_t* qh = a.q + ((size_t)b * a.Hq + (size_t)hkv * a.G) * a.Sq * D;
+  const size_t head_stride = (size_t)a.Sq * D;
+
+  const int c = lane & 15, kg = lane >> 4;
+  // Summaries of AHEAD tiles of the wave from block n0 on. The first are requested
+  // before the sequence's length is there.
+  auto fetch = [&](int n0, u32x4_t (&x)[AHEAD][KS]) {
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const uint16_t* sp = sh + (size_t)min(n0 + j * NW * 16 + c, a.NB - 1) * D + 8 * kg;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) x[j][k] = *reinterpret_cast<const u32x4_t*>(sp + 32 * k);
+    }
+  };
+  auto queries = [&](int pass, u32x4_t (&x)[CT][KS]) {
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+      const int p = a.per > 1 ? 0 : (t * 16 + c) / a.gp;
+      const int g = a.per > 1 ? pass * 16 + c : c % a.gp;
+      const uint16_t* qp =
+          qh + min(g, a.G - 1) * head_stride + (size_t)(p0 + min(p, npos - 1)) * D + 8 * kg;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) x[t][k] = *reinterpret_cast<const u32x4_t*>(qp + 32 * k);
+    }
+  };
+  u32x4_t next[AHEAD][KS], qf[CT][KS];
+  if (a.NB > 0) fetch(wave * 16, next);
+  queries(0, qf);
+
+  const int len = sequence_length(a.lengths, b, a.Skv);
   const long long diag0 = (long long)p0 + len - a.Sq;  // key of the first position
   auto own_block = [&](int p) {  // -1: before the first key
     const long long d = diag0 + p;
     return d < 0 ? -1 : (int)(d >> a.shift);
   };
-  const uint16_t* sh = a.s + (size_t)bh * a.NB * D;
-  const uint16_t* qh = a.q + ((size_t)b * a.Hq + (size_t)hkv * a.G) * a.Sq * D;
-  const size_t head_stride = (size_t)a.Sq * D;
-
   // Blocks that some position of the workgroup scores: below the last one's own.
   const int last = own_block(npos - 1);
   const int scored = last + 1 > a.K ? min(last - a.local + 1, a.NB) : 0;
   // Squares of the largest norms; the floor keeps the bound above what underflows.
-  float mnorm = 1e-36f, qnorm = 1e-36f;
-  uint32_t mbits = 0;  // whether some summary is not 0
+  constexpr float kTinyNorm = 1e-36f;
+  float mnorm = 0.f, qnorm = kTinyNorm;
   if (scored > 0) {
-    const int c = lane & 15, kg = lane >> 4;
+    auto norm2 = [](const u32x4_t (&x)[KS]) {  // of the lane's row (query or summary)
+      float n2 = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) n2 = dot2_bf16(x[k][e], x[k][e], n2);
+      float u, v;
+      lane_pair<16>(n2, u, v);
+      lane_pair<32>(u + v, u, v);
+      return u + v;
+    };
     for (int pass = 0; pass < a.per; ++pass) {
-      bf16x8_t qf[CT][KS];
-#pragma unroll
-      for (int t = 0; t < CT; ++t) {
-        const int p = a.per > 1 ? 0 : (t * 16 + c) / a.gp;
-        const int g = a.per > 1 ? pass * 16 + c : c % a.gp;
-        const uint16_t* qp =
-            qh + min(g, a.G - 1) * head_stride + (size_t)(p0 + min(p, npos - 1)) * D;
-        float n2 = 0.f;
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const u32x4_t x = *reinterpret_cast<const u32x4_t*>(qp + 32 * k + 8 * kg);
-          qf[t][k] = __builtin_bit_cast(bf16x8_t, x);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) n2 = dot2_bf16(x[e], x[e], n2);
-        }
-        float u, v;
-        lane_pair<16>(n2, u, v);
-        lane_pair<32>(u + v, u, v);
-        qnorm = fmaxf(qnorm, u + v);
+      if (pass > 0) {
+        fetch(wave * 16, next);
+        queries(pass, qf);
       }
-      for (int n0 = wave * 16; n0 < scored; n0 += NW * 16) {
-        const uint16_t* sp = sh + (size_t)min(n0 + c, a.NB - 1) * D + 8 * kg;
-        bf16x8_t sf[KS];
-        float n2 = 0.f;
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const u32x4_t x = *reinterpret_cast<const u32x4_t*>(sp + 32 * k);
-          sf[k] = __builtin_bit_cast(bf16x8_t, x);
+      for (int t = 0; t < CT; ++t) qnorm = fmaxf(qnorm, norm2(qf[t]));
+      for (int n0 = wave * 16; n0 < scored; n0 += AHEAD * NW * 16) {
+        u32x4_t sf[AHEAD][KS];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            n2 = dot2_bf16(x[e], x[e], n2);
-            mbits |= x[e];
-          }
-        }
-        float u, v;
-        lane_pair<16>(n2, u, v);
-        lane_pair<32>(u + v, u, v);
-        mnorm = fmaxf(mnorm, u + v);
+        for (int j = 0; j < AHEAD; ++j)
 #pragma unroll
-        for (int t = 0; t < CT; ++t) {
-          floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+          for (int k = 0; k < KS; ++k) sf[j][k] = next[j][k];
+        if (n0 + AHEAD * NW * 16 < scored) fetch(n0 + AHEAD * NW * 16, next);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+          const int n = n0 + j * NW * 16 + c;  // this lane's block
+          if (AHEAD > 1 && n0 + j * NW * 16 >= scored) break;
+          mnorm = fmaxf(mnorm, norm2(sf[j]));
+          floatx4 acc[CT];
+#pragma unroll
+          for (int t = 0; t < CT; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int k = 0; k < KS; ++k)
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sf[k], qf[t][k], acc, 0, 0, 0);
-          // Lane: column c, blocks n0 + 4 kg + i.
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float x = acc[i] == acc[i] ? acc[i] : kNegInf;
-            if (a.gp > 1) x = fmaxf(x, dpp_mov<kDppQuadXor1>(x));
-            if (a.gp > 2) x = fmaxf(x, dpp_mov<kDppQuadXor2>(x));
-            if (a.gp > 4) x = fmaxf(x, dpp_mov<kDppHalfMirror>(x));
-            if (a.gp > 8) x = fmaxf(x, dpp_mov<kDppRowRor8>(x));
-            acc[i] = x;
-          }
-          const int p = a.per > 1 ? 0 : (t * 16 + c) / a.gp;
-          if (c % a.gp == 0 && p < npos) {
-            float4* dst = reinterpret_cast<float4*>(scores + p * a.stride + n0 + 4 * kg);
-            float4 x = make_float4(acc[0], acc[1], acc[2], acc[3]);
-            if (pass > 0) {  // the same lane wrote the earlier heads' maximum
-              const float4 y = *dst;
-              x = make_float4(fmaxf(x.x, y.x), fmaxf(x.y, y.y), fmaxf(x.z, y.z), fmaxf(x.w, y.w));
+            for (int t = 0; t < CT; ++t)
+              acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  __builtin_bit_cast(bf16x8_t, qf[t][k]), __builtin_bit_cast(bf16x8_t, sf[j][k]),
+                  acc[t], 0, 0, 0);
+          // Lane: block n, rows 4 kg + i of each tile. The maxima pass over a NaN.
+#pragma unroll
+          for (int t = 0; t < CT; ++t) {
+            if (a.gp >= 4) {
+              float x = fmaxf(fmaxf(acc[t][0], acc[t][1]), fmaxf(acc[t][2], acc[t][3]));
+              float u, v;
+              if (a.gp >= 8) {
+                lane_pair<16>(x, u, v);
+                x = fmaxf(u, v);
+              }
+              if (a.gp >= 16) {
+                lane_pair<32>(x, u, v);
+                x = fmaxf(u, v);
+              }
+              const int p = a.per > 1 ? 0 : (t * 16 + 4 * kg) / a.gp;
+              if ((4 * kg) % a.gp == 0 && p < npos) {
+                float* dst = scores + p * a.stride + n;
+                *dst = pass > 0 ? fmaxf(x, *dst) : x;  // the same lane wrote *dst
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int p = (t * 16 + 4 * kg + i) / a.gp;
+                const float x = a.gp == 2 ? fmaxf(acc[t][i], acc[t][i ^ 1]) : acc[t][i];
+                if (i % a.gp == 0 && p < npos) scores[p * a.stride + n] = x;
+              }
             }
-            *dst = x;
           }
         }
       }
     }
     mnorm = wave_max(mnorm);
     qnorm = wave_max(qnorm);
-    const bool any = __ballot((mbits & 0x7fff7fffu) != 0) != 0;
+    uint32_t bits = 1;
+    if (mnorm == 0.f) {  // zeros, or too small for their squares
+      bits = 0;
+      for (int n0 = wave * 16; n0 < scored; n0 += NW * 16) {
+        const uint32_t* sp = reinterpret_cast<const uint32_t*>(sh + (size_t)n0 * D);
+        const int words = min(16, a.NB - n0) * (D / 2);
+        for (int i = lane; i < words; i += 64) bits |= sp[i] & 0x7fff7fffu;
+      }
+    }
+    const bool any = __ballot(bits != 0) != 0;
     if (lane == 0) {
-      norms[wave] = mnorm;
+      norms[wave] = fmaxf(mnorm, kTinyNorm);
       nonzero[wave] = any;
     }
   }
@@ -271,99 +614,34 @@ __global__ __launch_bounds__(NW * 64) void block_select_kernel(SelectParams a) {
       for (int i = lane; i < a.K; i += 64) out[i] = i <= cur ? i : -1;
       continue;
     }
-    float* sc = scores + p * a.stride;
     const int c0 = a.sinks, c1 = cur - a.local + 1;
-    const int need = a.K - a.sinks - a.local;  // below c1 - c0
-    float thr = -kNegInf;  // blocks of [c0, c1) with a score >= thr are taken
-    bool none = need == 0;
-    if (!none) {
-      uint32_t T = 0;
-      int cnt = c1 - c0;
-      for (int bit = 31; bit >= 0 && cnt != need; --bit) {
-        const uint32_t cand = T | (1u << bit);
-        int k = 0;
-        for (int base = c0; base < c1; base += 64) {
-          const int n = base + lane;
-          k += (int)__popcll(__ballot(n < c1 && ordered(sc[min(n, c1 - 1)]) >= cand));
-        }
-        if (k >= need) {
-          T = cand;
-          cnt = k;
-        }
-      }
-      // Last score in, first one out.
-      float in = -kNegInf, outv = kNegInf;
-      for (int n = c0 + lane; n < c1; n += 64) {
-        const float x = sc[n];
-        if (ordered(x) >= T) in = fminf(in, x);
-        else outv = fmaxf(outv, x);
-      }
-      in = wave_min(in);
-      outv = wave_max(outv);
-      if (cnt != need) outv = in;
-      // (in = -inf adds nothing; an infinite bound stays infinite.)
-      const float e2 = 2.f * bound + (in == kNegInf ? 0.f : 4.8e-7f * fabsf(in)) + 1e-30f;
-      thr = in;
-      if (!(in - outv > e2)) {
-        // Scores that are -inf (NaN), or 0 because all summaries or all of the
-        // position's queries are, need no second look: their indices decide.
-        const bool finite = e2 < -kNegInf;
-        const bool settled = (finite && in == kNegInf) || !summaries ||
-                             all_zero<D>(qh + (size_t)(p0 + p) * D, head_stride, a.G);
-        const float lo = settled ? in : finite ? in - e2 : kNegInf;
-        const float hi = settled ? in : finite ? in + e2 : -kNegInf;
-        int sure = 0;
-        for (int base = c0; base < c1; base += 64) {
-          const int n = base + lane;
-          sure += (int)__popcll(__ballot(n < c1 && sc[min(n, c1 - 1)] > hi));
-        }
-        int want = need - sure;
-        if (settled) {
-          for (int base = c0; base < c1; base += 64) {
-            const int n = base + lane;
-            const bool tie = n < c1 && sc[min(n, c1 - 1)] == in;
-            const unsigned long long m = __ballot(tie);
-            const int rank = (int)__popcll(m & ((1ull << lane) - 1));
-            if (tie) sc[n] = rank < want ? -kNegInf : kNegInf;
-            want = max(want - (int)__popcll(m), 0);
-          }
-          wave_lds_sync();
-          thr = in == kNegInf ? -3.402823466e+38f : in;
-        } else {
-          settle_border<D>(sc, c0, c1, lo, hi, want, qh + (size_t)(p0 + p) * D, head_stride, a.G,
-                           sh);
-          thr = hi;
-        }
-      }
-    }
-    int at = 0;
-    for (int base = 0; base <= cur; base += 64) {
-      const int n = base + lane;
-      const bool take = n <= cur && (n < c0 || n >= c1 || (!none && sc[n] >= thr));
-      const unsigned long long m = __ballot(take);
-      const int slot = at + (int)__popcll(m & ((1ull << lane) - 1));
-      if (take && slot < a.K) out[slot] = n;
-      at += (int)__popcll(m);
-    }
+    const Choice ch{(lds_float*)(scores + p * a.stride), c0, c1, a.K - c0 - a.local, bound,
+                    summaries, qh + (size_t)(p0 + p) * D, head_stride, a.G, sh, out + c0};
+    for (int i = lane; i < c0; i += 64) out[i] = i;
+    for (int i = c1 + lane; i <= cur; i += 64) out[a.K - 1 - (cur - i)] = i;
+    if (ch.need == 0) continue;
+    lds_u64* const words = (lds_u64*)scratch[wave];
+    const bool done = c1 - c0 <= 64 * 4    ? choose_few<D, 4>(ch, words)
+                      : c1 - c0 <= 64 * 16 ? choose_few<D, 16>(ch, words)
+                                           : choose_few<D, 0>(ch, words);
+    if (!done) choose_many<D>(ch);
   }
 }
 
-constexpr int kSelectWaves = 8;
-
-template <int D, int CT>
-hipError_t launch_ct(const SelectParams& a, hipStream_t stream) {
-  const size_t lds = (size_t)a.pos * a.stride * sizeof(float);
-  hipLaunchKernelGGL((block_select_kernel<D, CT, kSelectWaves>),
-                     dim3((unsigned)a.B * a.Hkv * a.ptiles), dim3(kSelectWaves * 64), lds, stream,
-                     a);
+template <int D, int CT, int NW, int AHEAD, int LDS>
+hipError_t launch_one(const SelectParams& a, hipStream_t stream) {
+  const size_t lds = LDS > 0 ? 0 : (size_t)a.pos * a.stride * sizeof(float);
+  hipLaunchKernelGGL((block_select_kernel<D, CT, NW, AHEAD, LDS>),
+                     dim3((unsigned)a.B * a.Hkv * a.ptiles), dim3(NW * 64), lds, stream, a);
   return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_d(const SelectParams& a, hipStream_t stream) {
-  const int columns = a.per > 1 ? 16 : a.pos * a.gp;
-  if (columns <= 16) return launch_ct<D, 1>(a, stream);
-  return launch_ct<D, 4>(a, stream);
+  const int rows = a.per > 1 ? 16 : a.pos * a.gp;
+  if (rows > 16) return launch_one<D, 4, 4, 2, kSelectLds / 4>(a, stream);
+  if (a.waves == 8) return launch_one<D, 1, 8, 4, 0>(a, stream);
+  return launch_one<D, 1, 4, 2, 0>(a, stream);
 }
 
 }  // namespace

@@ -29,6 +29,10 @@ struct SummaryParams {
   int touched;   // blocks per (sequence, head) that the launch looks at
 };
 
+// Bytes of LDS for the scores of a selection workgroup of many rows: two to a compute
+// unit. With few rows the launch sets the size, 64 KiB at most.
+constexpr int kSelectLds = 74 * 1024;
+
 struct SelectParams {
   const uint16_t* q;   // [B][Hq][Sq][D] bf16
   const uint16_t* s;   // [B][Hkv][NB][D] bf16
@@ -39,9 +43,10 @@ struct SelectParams {
   int NB;
   int shift;     // log2 of the keys per block
   int K, sinks, local;
-  // Columns of the score product: a position takes gp columns (G rounded up to a
-  // power of two, at most 16) of a 16-column tile, or `per` whole tiles when G > 16.
+  // Rows of the score product: a position takes gp rows (G rounded up to a power of
+  // two, at most 16) of a 16-row tile, or `per` whole tiles when G > 16.
   int gp, per;
+  int waves;     // waves per workgroup where its rows fill one tile: 4 or 8
   int pos;       // positions per workgroup
   int ptiles;    // workgroups per (sequence, head)
   int stride;    // floats of a position's score row in LDS

@@ -22,9 +22,8 @@ int num_blocks(int Skv, int block_size) {
   return nb <= ef::kMaxBlocks ? nb : -1;
 }
 
-// Most bytes of LDS a selection workgroup keeps its scores in: two workgroups to
-// a compute unit, and any list of EF_MAX_BLOCKS scores fits.
-constexpr int kSelectLds = 64 * 1024 - 256;
+// Most bytes of LDS a launch may ask for: any list of EF_MAX_BLOCKS scores fits.
+constexpr int kLaunchLds = 64 * 1024;
 
 }  // namespace
 
@@ -85,15 +84,19 @@ ef_status ef_block_select(const void* q, const void* summary, const int* lengths
   a.gp = 1;
   while (a.gp < a.G && a.gp < 16) a.gp *= 2;
   a.per = (a.G + 15) / 16;
-  // Rows of four floats more than whole tiles: 16 positions' rows start in different banks.
+  // Rows of four floats more than whole tiles: the rows of a tile's positions start in
+  // different banks.
   a.stride = (nb + 15) / 16 * 16 + 4;
-  // Positions per workgroup: four column tiles where the scores fit and the grid
-  // still fills the chip, else one tile, fewer positions where they do not fit.
+  // Positions per workgroup: four row tiles where at least three of them have a
+  // position's scores to keep and the grid still fills the chip, else one tile, fewer
+  // positions where they do not fit.
   const long long heads = (long long)B * Hkv;
-  const int fit = std::max(1, kSelectLds / (a.stride * 4));
-  int pos = a.per > 1 ? 1 : 16 / a.gp;
-  if (a.per == 1 && 4 * pos <= fit && heads * ((Sq + 4 * pos - 1) / (4 * pos)) >= 512) pos *= 4;
-  a.pos = std::min(std::min(pos, fit), Sq);
+  const int row = a.stride * 4, tile = a.per > 1 ? 1 : 16 / a.gp;
+  a.pos = std::min(std::min(tile, std::max(1, kLaunchLds / row)), Sq);
+  const int wide = std::min(4 * tile, ef::kSelectLds / row);
+  if (a.per == 1 && wide > 2 * tile && heads * ((Sq + wide - 1) / wide) >= 512) a.pos = wide;
+  // Eight waves share the blocks of a workgroup where the grid leaves room for them.
+  a.waves = heads * ((Sq + a.pos - 1) / a.pos) <= 256 ? 8 : 4;
   const long long ptiles = ((long long)Sq + a.pos - 1) / a.pos;
   if (heads * ptiles >= (1LL << 31)) return EF_ERR_INVALID_SHAPE;
   a.ptiles = (int)ptiles;
