@@ -40,6 +40,7 @@ namespace {
 // -> ?).
 typedef __attribute__((address_space(3))) float lds_float;
 typedef __attribute__((address_space(3))) unsigned long long lds_u64;
+typedef __attribute__((address_space(3))) u32x4_t lds_chunk;
 
 // Order-preserving integer of a float (no NaN).
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -457,6 +458,7 @@ void block_select_kernel(SelectParams a) {
   extern __shared__ __align__(16) float launch_lds[];
   __shared__ __align__(16) float fixed_lds[LDS > 0 ? LDS : 4];
   float* const scores = LDS > 0 ? fixed_lds : launch_lds;  // [pos][stride]
+  __shared__ __align__(16) u32x4_t tiles[NW][128];
   __shared__ unsigned long long scratch[NW][66];
   __shared__ float norms[NW];
   __shared__ uint32_t nonzero[NW];
@@ -474,10 +476,30 @@ void block_select_kernel(SelectParams a) {
   // before the sequence's length is there.
   auto fetch = [&](int n0, u32x4_t (&x)[AHEAD][KS]) {
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) {
-      const uint16_t* sp = sh + (size_t)min(n0 + j * NW * 16 + c, a.NB - 1) * D + 8 * kg;
+    for (int j = 0; j < AHEAD; ++j)
 #pragma unroll
-      for (int k = 0; k < KS; ++k) x[j][k] = *reinterpret_cast<const u32x4_t*>(sp + 32 * k);
+      for (int k = 0; k < KS; ++k) {
+        const int n = n0 + j * NW * 16 + (k & 1) * 8 + (lane >> 3);
+        const uint16_t* sp = sh + (size_t)min(n, a.NB - 1) * D + (k >> 1) * 64 + (lane & 7) * 8;
+        x[j][k] = *reinterpret_cast<const u32x4_t*>(sp);
+      }
+  };
+  // The lane's part of a tile as the product takes it: block c, elements 32 k + 8 kg on.
+  // A load covers eight blocks' 128-byte lines (16 blocks to a quarter of a wave cost
+  // the address unit a lookup a lane, 16 a load instead of 2: ?).
+  // The 64-element halves of a tile turn in a 2 KiB buffer of the wave, 16-byte chunks
+  // permuted by row against bank conflicts; LDS keeps a wave's operations in order.
+  auto turn = [&](const u32x4_t (&x)[KS], u32x4_t (&y)[KS]) {
+    lds_chunk* const buf = (lds_chunk*)tiles[wave];
+#pragma unroll
+    for (int half = 0; half < KS / 2; ++half) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        buf[(i * 8 + (lane >> 3)) * 8 + ((lane & 7) ^ (lane >> 3))] = x[2 * half + i];
+      wave_lds_sync();
+#pragma unroll
+      for (int i = 0; i < 2; ++i) y[2 * half + i] = buf[c * 8 + ((4 * i + kg) ^ (c & 7))];
+      wave_lds_sync();
     }
   };
   auto queries = [&](int pass, u32x4_t (&x)[CT][KS]) {
@@ -519,65 +541,81 @@ void block_select_kernel(SelectParams a) {
       lane_pair<32>(u + v, u, v);
       return u + v;
     };
-    for (int pass = 0; pass < a.per; ++pass) {
-      if (pass > 0) {
-        fetch(wave * 16, next);
-        queries(pass, qf);
-      }
+    // The score rows for GP rows to a position, in `per` passes where GP is 16. Rows of
+    // the tiles without a position of their own repeat the last one, and lanes that
+    // share a maximum write it to the same word, so no write needs a condition.
+    auto score = [&](auto gp_tag) {
+      constexpr int GP = decltype(gp_tag)::value;
+      constexpr int PER = GP < 4 ? 4 / GP : 1;  // positions among a lane's four rows
+      lds_float* row[CT][PER];
 #pragma unroll
-      for (int t = 0; t < CT; ++t) qnorm = fmaxf(qnorm, norm2(qf[t]));
-      for (int n0 = wave * 16; n0 < scored; n0 += AHEAD * NW * 16) {
-        u32x4_t sf[AHEAD][KS];
+      for (int t = 0; t < CT; ++t)
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j)
+        for (int i = 0; i < PER; ++i) {
+          const int p = a.per > 1 ? 0 : (t * 16 + 4 * kg + i * GP) / GP;
+          row[t][i] = (lds_float*)(scores + min(p, npos - 1) * a.stride + c);
+        }
+      for (int pass = 0; pass < (GP == 16 ? a.per : 1); ++pass) {
+        if (pass > 0) {
+          fetch(wave * 16, next);
+          queries(pass, qf);
+        }
 #pragma unroll
-          for (int k = 0; k < KS; ++k) sf[j][k] = next[j][k];
-        if (n0 + AHEAD * NW * 16 < scored) fetch(n0 + AHEAD * NW * 16, next);
+        for (int t = 0; t < CT; ++t) qnorm = fmaxf(qnorm, norm2(qf[t]));
+        for (int n0 = wave * 16; n0 < scored; n0 += AHEAD * NW * 16) {
+          u32x4_t now[AHEAD][KS];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-          const int n = n0 + j * NW * 16 + c;  // this lane's block
-          if (AHEAD > 1 && n0 + j * NW * 16 >= scored) break;
-          mnorm = fmaxf(mnorm, norm2(sf[j]));
-          floatx4 acc[CT];
+          for (int j = 0; j < AHEAD; ++j)
 #pragma unroll
-          for (int t = 0; t < CT; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < KS; ++k) now[j][k] = next[j][k];
+          if (n0 + AHEAD * NW * 16 < scored) fetch(n0 + AHEAD * NW * 16, next);
 #pragma unroll
-          for (int k = 0; k < KS; ++k)
+          for (int j = 0; j < AHEAD; ++j) {
+            const int n = n0 + j * NW * 16;  // first block of the tile
+            if (AHEAD > 1 && n >= scored) break;
+            u32x4_t sf[KS];
+            turn(now[j], sf);
+            mnorm = fmaxf(mnorm, norm2(sf));
+            floatx4 acc[CT];
+#pragma unroll
+            for (int t = 0; t < CT; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+              for (int t = 0; t < CT; ++t)
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    __builtin_bit_cast(bf16x8_t, qf[t][k]), __builtin_bit_cast(bf16x8_t, sf[k]),
+                    acc[t], 0, 0, 0);
+            // Lane: block n + c, rows 4 kg + i of each tile. The maxima pass over a NaN.
 #pragma unroll
             for (int t = 0; t < CT; ++t)
-              acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                  __builtin_bit_cast(bf16x8_t, qf[t][k]), __builtin_bit_cast(bf16x8_t, sf[j][k]),
-                  acc[t], 0, 0, 0);
-          // Lane: block n, rows 4 kg + i of each tile. The maxima pass over a NaN.
 #pragma unroll
-          for (int t = 0; t < CT; ++t) {
-            if (a.gp >= 4) {
-              float x = fmaxf(fmaxf(acc[t][0], acc[t][1]), fmaxf(acc[t][2], acc[t][3]));
-              float u, v;
-              if (a.gp >= 8) {
-                lane_pair<16>(x, u, v);
-                x = fmaxf(u, v);
-              }
-              if (a.gp >= 16) {
-                lane_pair<32>(x, u, v);
-                x = fmaxf(u, v);
-              }
-              const int p = a.per > 1 ? 0 : (t * 16 + 4 * kg) / a.gp;
-              if ((4 * kg) % a.gp == 0 && p < npos) {
-                float* dst = scores + p * a.stride + n;
-                *dst = pass > 0 ? fmaxf(x, *dst) : x;  // the same lane wrote *dst
-              }
-            } else {
+              for (int i = 0; i < PER; ++i) {
+                float x = acc[t][i * (4 / PER)];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int p = (t * 16 + 4 * kg + i) / a.gp;
-                const float x = a.gp == 2 ? fmaxf(acc[t][i], acc[t][i ^ 1]) : acc[t][i];
-                if (i % a.gp == 0 && p < npos) scores[p * a.stride + n] = x;
+                for (int e = 1; e < 4 / PER; ++e) x = fmaxf(x, acc[t][i * (4 / PER) + e]);
+                float u, v;
+                if constexpr (GP >= 8) {
+                  lane_pair<16>(x, u, v);
+                  x = fmaxf(u, v);
+                }
+                if constexpr (GP >= 16) {
+                  lane_pair<32>(x, u, v);
+                  x = fmaxf(u, v);
+                  if (pass > 0) x = fmaxf(x, row[t][i][n]);
+                }
+                row[t][i][n] = x;
               }
-            }
           }
         }
       }
+    };
+    switch (a.gp) {
+      case 1: score(std::integral_constant<int, 1>{}); break;
+      case 2: score(std::integral_constant<int, 2>{}); break;
+      case 4: score(std::integral_constant<int, 4>{}); break;
+      case 8: score(std::integral_constant<int, 8>{}); break;
+      default: score(std::integral_constant<int, 16>{}); break;
     }
     mnorm = wave_max(mnorm);
     qnorm = wave_max(qnorm);
@@ -640,7 +678,7 @@ template <int D>
 hipError_t launch_d(const SelectParams& a, hipStream_t stream) {
   const int rows = a.per > 1 ? 16 : a.pos * a.gp;
   if (rows > 16) return launch_one<D, 4, 4, 2, kSelectLds / 4>(a, stream);
-  if (a.waves == 8) return launch_one<D, 1, 8, 4, 0>(a, stream);
+  if (a.waves == 8) return launch_one<D, 1, 8, 2, 0>(a, stream);
   return launch_one<D, 1, 4, 2, 0>(a, stream);
 }
 

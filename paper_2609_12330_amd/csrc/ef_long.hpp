@@ -31,7 +31,7 @@ struct SummaryParams {
 
 // Bytes of LDS for the scores of a selection workgroup of many rows: two to a compute
 // unit. With few rows the launch sets the size, 64 KiB at most.
-constexpr int kSelectLds = 74 * 1024;
+constexpr int kSelectLds = 66 * 1024;
 
 struct SelectParams {
   const uint16_t* q;   // [B][Hq][Sq][D] bf16
