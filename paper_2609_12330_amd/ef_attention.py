@@ -628,15 +628,22 @@ def attention_decode_dsplit(q, k, v, scale: Optional[float] = None, causal: bool
 # ---------------------------------------------------------------------------
 
 
+# These checks are on the path of every call too: the conditions are tested together, on the
+# cheap device index, and only a call that breaks one goes through them by name.
+
+
 def _check_tensor(t, name, dtype, dim, ref=None):
-    """A contiguous GPU tensor of this type and number of axes, on `ref`'s device."""
+    """Raises unless t is a contiguous GPU tensor of this type and number of axes, on `ref`'s
+    device."""
+    if (t.dtype is dtype and t.dim() == dim and t.is_contiguous() and
+            (t.is_cuda if ref is None else t.get_device() == ref.get_device())):
+        return
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_cuda or (ref is not None and t.device != ref.device):
         raise TypeError(f"{name} must be a GPU tensor" +
                         (f" on {ref.device}, got {t.device}" if ref is not None else ""))
-    if t.dim() != dim or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dim}-D tensor")
+    raise ValueError(f"{name} must be a contiguous {dim}-D tensor")
 
 
 def _lengths_ptr(lengths, B, ref):
@@ -648,15 +655,22 @@ def _lengths_ptr(lengths, B, ref):
     return lengths.data_ptr()
 
 
+def _current_device():
+    c = _torch()._C
+    try:
+        return c._cuda_getDevice()
+    except AttributeError:  # not a public name either
+        return _torch().cuda.current_device()
+
+
 def _call_on(t, stream, fn, *args):
     """fn(*args, stream handle) with t's device current: a launch needs the device of its
     stream, and the current stream of another device is not the one t's work is ordered on."""
-    torch = _torch()
     if stream is not None and stream.device != t.device:
         raise ValueError(f"stream is on {stream.device}, the tensors are on {t.device}")
-    if torch.cuda.current_device() == t.device.index:
+    if _current_device() == t.get_device():
         return fn(*args, _stream_handle(stream))
-    with torch.cuda.device(t.device):
+    with _torch().cuda.device(t.device):
         return fn(*args, _stream_handle(stream))
 
 
@@ -720,6 +734,12 @@ def block_select(q, summary, Skv: int, topk: int, block_size: int = 64, sink_blo
     return out
 
 
+def _same_devices(q, k, v):
+    if q.get_device() != k.get_device() or q.get_device() != v.get_device():
+        _same_device(k, q, "k")
+        _same_device(v, q, "v")
+
+
 def _out_bf16(q, out):
     torch = _torch()
     if out is None:
@@ -730,15 +750,16 @@ def _out_bf16(q, out):
     return out
 
 
-def _own_workspace(workspace, size, q):
-    """(pointer, bytes) of the workspace given, or of a new one of size() bytes."""
+def _own_workspace(workspace, size, sizes, q):
+    """(pointer, bytes, tensor) of the workspace given, or of a new one of size(*sizes) bytes."""
     if workspace is None:
-        n = size()
+        n = size(*sizes)
         if n == 0:
             return None, 0, None
         workspace = _torch().empty(n, dtype=_torch().uint8, device=q.device)
-    _check_workspace(workspace, q)
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+    if workspace.get_device() != q.get_device() or not workspace.is_contiguous():
+        _check_workspace(workspace, q)
+    return workspace.data_ptr(), workspace.nbytes, workspace
 
 
 def make_blocks_workspace(q, k, topk: int, block_size: int = 64):
@@ -756,8 +777,7 @@ def attention_blocks(q, k, v, blocks, block_size: int = 64, scale: Optional[floa
     shaped like q."""
     torch = _torch()
     B, Hq, Hkv, Sq, Skv, D = _check_qkv(q, k, v)
-    for name, t in (("k", k), ("v", v)):
-        _same_device(t, q, name)
+    _same_devices(q, k, v)
     _check_tensor(blocks, "blocks", torch.int32, 4, q)
     topk = blocks.shape[3]
     if blocks.shape[:3] != (B, Hkv, Sq):
@@ -766,8 +786,8 @@ def attention_blocks(q, k, v, blocks, block_size: int = 64, scale: Optional[floa
         scale = 1.0 / math.sqrt(D)
     o = _out_bf16(q, out)
     ptr, n, workspace = _own_workspace(
-        workspace, lambda: ef_attention_blocks_workspace_size(B, Hq, Hkv, Sq, Skv, D, block_size,
-                                                              topk), q)
+        workspace, ef_attention_blocks_workspace_size, (B, Hq, Hkv, Sq, Skv, D, block_size, topk),
+        q)
     st = _call_on(q, stream, ef_attention_blocks, q.data_ptr(), k.data_ptr(), v.data_ptr(),
                   blocks.data_ptr(), _lengths_ptr(lengths, B, q), o.data_ptr(), B, Hq, Hkv, Sq,
                   Skv, D, float(scale), block_size, topk, ptr, n)
@@ -791,8 +811,7 @@ def attention_shared_prefix(q, k_prefix, v_prefix, k, v, scale: Optional[float] 
     q."""
     torch = _torch()
     B, Hq, Hkv, Sq, Skv, D = _check_qkv(q, k, v)
-    for name, t in (("k", k), ("v", v)):
-        _same_device(t, q, name)
+    _same_devices(q, k, v)
     _check_tensor(k_prefix, "k_prefix", torch.bfloat16, 3, q)
     _check_tensor(v_prefix, "v_prefix", torch.bfloat16, 3, q)
     Lp = k_prefix.shape[1]
@@ -802,8 +821,7 @@ def attention_shared_prefix(q, k_prefix, v_prefix, k, v, scale: Optional[float] 
         scale = 1.0 / math.sqrt(D)
     o = _out_bf16(q, out)
     ptr, n, workspace = _own_workspace(
-        workspace, lambda: ef_attention_shared_prefix_workspace_size(B, Hq, Hkv, Sq, Lp, Skv, D),
-        q)
+        workspace, ef_attention_shared_prefix_workspace_size, (B, Hq, Hkv, Sq, Lp, Skv, D), q)
     st = _call_on(q, stream, ef_attention_shared_prefix, q.data_ptr(), k_prefix.data_ptr(),
                   v_prefix.data_ptr(), k.data_ptr(), v.data_ptr(), _lengths_ptr(lengths, B, q),
                   o.data_ptr(), B, Hq, Hkv, Sq, Lp, Skv, D, float(scale), causal, ptr, n)
