@@ -485,9 +485,13 @@ ef_status ef_block_select(const void* q, const void* summary, const int* lengths
  *   topk   : 1 .. EF_MAX_TOPK.
  *   o      : [B][Hq][Sq][D] bf16.
  *   workspace : ef_attention_blocks_workspace_size(...) bytes, 16-byte aligned (may
- *            be NULL where that is 0). It holds partial states during the call only
- *            and need not be cleared; calls that overlap in time must not share one,
- *            and neither must two captured graphs that may run at the same time.
+ *            be NULL where that is 0), with the counter region of
+ *            ef_attention_splitkv's workspace at its start: zero before the first
+ *            call that uses it, left zero by every completed call. One workspace
+ *            serves any number of calls of these and the split-KV entry points, in
+ *            stream order; calls that overlap in time must not share one, and neither
+ *            must two captured graphs that may run at the same time. Rows whose
+ *            counter was not zero are filled with NaN.
  * Work and traffic grow with the union of the lists of about 64 * Hkv / Hq neighbouring
  * queries, which is little more than one list where neighbours choose alike.
  * Errors: EF_ERR_INVALID_BLOCKS for block_size, NB or topk; others as for

@@ -38,6 +38,7 @@ struct ListTiles {
   int cend;     // keys any row sees
   int full_lo;  // keys up to it are visible to all rows, as far as selected
   int pos;      // bit of this lane's position
+  bool once;    // no other workgroup reads the keys: they stream past the caches
 
   __device__ __forceinline__ TileAt at(int t) const {
     const int per = shift - 6;
@@ -51,7 +52,10 @@ struct ListTiles {
   }
   template <bool ISK>
   __device__ __forceinline__ void load(char* stage, const TileAt& t) const {
-    ld.template load<ISK>(stage, t.base, t.end);
+    if (once)
+      ld.template load<ISK, 2>(stage, t.base, t.end);
+    else
+      ld.template load<ISK>(stage, t.base, t.end);
   }
 };
 
@@ -97,6 +101,7 @@ void attn_blocks_kernel(BlocksParams a) {
   tl.cend = s1 + off + 1;
   tl.full_lo = s0 + off;
   tl.pos = valid ? sq - s0 : 0;
+  tl.once = a.mtiles == 1;
 
   // Bitmap of the union: entries of the positions' lists, up to each one's own block.
   const int* lists = a.blocks + ((size_t)bh * a.Sq + s0) * a.K;
@@ -169,12 +174,23 @@ void attn_blocks_kernel(BlocksParams a) {
     const int tail = __builtin_amdgcn_readfirstlane(u.block[n - 1]);
     if (per && (tail << a.shift) + 64 >= tl.cend) --tiles;
     roll_tiles<D, SEL>(tl, tiles, mt * BM + wave * 32 < a.R, Stages{sk0, sk1, sv0, sv1}, fr, row,
-                       fmaxf(a.c_abs, 1e-30f), mask);
+                       fmaxf(a.c_abs, 1e-30f), mask, [] {});
   }
-  if (a.P == 1)
+  if (a.P == 1) {
     store_row<D>(row, h, valid ? a.o + orow * D : nullptr);
-  else
-    store_state<D>(row, h, valid, a.ws_m, a.ws_l, a.ws_acc, orow * a.P + p);
+    return;
+  }
+  const bool shared = a.counters != nullptr;
+  store_state<D>(row, h, valid, a.ws_m, a.ws_l, a.ws_acc, orow * a.P + p, shared);
+  if (!shared) return;
+  // The last part of the head's rows to arrive combines them.
+  unsigned* const counter = a.counters + (size_t)bh * kCounterStride;
+  const size_t row0 = (size_t)bh * a.R;
+  const unsigned ticket = arrival_ticket(counter);
+  if (ticket >= (unsigned)a.P) poison_rows<D, NT>(a.o, row0, a.R);
+  if (ticket != (unsigned)(a.P - 1)) return;
+  combine_shared<D, NT>(a.ws_m, a.ws_l, a.ws_acc, a.o, row0, a.R, a.P);
+  if (threadIdx.x == 0) reset_counter(counter);
 }
 
 template <int D, int NW>

@@ -28,6 +28,7 @@ struct TwoRuns {
   int first;                          // first tile of the walk
   int np, Lp, end;                    // prefix tiles and keys, all keys
   int full_lo;                        // keys up to it are visible to all rows of the wave
+  bool once;                          // no other workgroup reads the keys of the walk
 
   __device__ __forceinline__ TileAt at(int t) const {
     t += first;
@@ -45,15 +46,27 @@ struct TwoRuns {
     StageLoader<D, NW, NW> l = ld;
     auto& rs = ISK ? l.krs : l.vrs;
     rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p), (short)0, -1, 0x00020000);
-    l.template load<ISK>(stage, t.base - off, t.end - off);
+    if (once)
+      l.template load<ISK, 2>(stage, t.base - off, t.end - off);
+    else
+      l.template load<ISK>(stage, t.base - off, t.end - off);
   }
 };
 
-// Smallest value of x over the wave.
+// Smallest value of x over the wave, in DPP moves and lane swaps.
 __device__ __forceinline__ int wave_min_int(int x) {
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) x = min(x, __shfl_xor(x, m, 64));
-  return __builtin_amdgcn_readfirstlane(x);
+  auto mov = [](int v, auto ctrl) {
+    return __float_as_int(dpp_mov<decltype(ctrl)::value>(__int_as_float(v)));
+  };
+  x = min(x, mov(x, std::integral_constant<int, kDppQuadXor1>{}));
+  x = min(x, mov(x, std::integral_constant<int, kDppQuadXor2>{}));
+  x = min(x, mov(x, std::integral_constant<int, kDppHalfMirror>{}));
+  x = min(x, mov(x, std::integral_constant<int, kDppRowRor8>{}));
+  float a, b;
+  lane_pair<16>(__int_as_float(x), a, b);
+  x = min(__float_as_int(a), __float_as_int(b));
+  lane_pair<32>(__int_as_float(x), a, b);
+  return __builtin_amdgcn_readfirstlane(min(__float_as_int(a), __float_as_int(b)));
 }
 
 template <int D, int NW>
@@ -87,11 +100,6 @@ void attn_prefix_kernel(PrefixParams a) {
   const int rr = valid ? (packed ? r % a.R : r) : 0;
   const int sq = rr / a.G, g = rr % a.G;
   const size_t orow = ((size_t)b * a.Hq + (size_t)hkv * a.G + g) * a.Sq + sq;
-  const int all_u = a.Lp + sequence_length(a.lengths, bu, a.Skv);
-  const int all = packed ? a.Lp + sequence_length(a.lengths, b, a.Skv) : all_u;
-  // Last key the row sees; all of them without a mask.
-  const int lim = !valid ? -1 : a.causal ? sq + all - a.Sq : 0x7fffffff;
-
   // Tiles of 64 keys of the walk.
   TwoRuns<D, NW> tl;
   tl.Lp = a.Lp;
@@ -101,16 +109,17 @@ void attn_prefix_kernel(PrefixParams a) {
   const size_t own = ((size_t)bu * a.Hkv + hkv) * (size_t)a.Skv * D;
   tl.ko = packed ? tl.kp : a.k + own;
   tl.vo = packed ? tl.vp : a.v + own;
-  tl.full_lo = wave_min_int(valid ? lim : 0x7fffffff);
+  tl.once = packed ? a.mt1 == 1 : a.mt2 == 1 && !a.whole;
   int last;
   if (packed) {
     tl.end = a.Lp;
     tl.first = p * a.T1;
     last = min(tl.first + a.T1, tl.np);
   } else {
+    const int all = a.Lp + sequence_length(a.lengths, bu, a.Skv);  // (checked on the host)
     // Keys behind the last row's are not visited.
     const int top = min(mt * BM + BM, rows) - 1;
-    const int seen = a.causal ? min(all_u, top / a.G + all_u - a.Sq + 1) : all_u;
+    const int seen = a.causal ? min(all, top / a.G + all - a.Sq + 1) : all;
     tl.end = max(seen, 0);
     const int tiles = tl.end <= a.Lp ? (tl.end + 63) / 64 : tl.np + (tl.end - a.Lp + 63) / 64;
     tl.first = a.whole ? 0 : tl.np + p * a.T2;
@@ -124,15 +133,22 @@ void attn_prefix_kernel(PrefixParams a) {
   constexpr int STAGE = 2 * Geo::SUB;
   __shared__ __align__(1024) char sk0[STAGE], sk1[STAGE], sv0[STAGE], sv1[STAGE];
   tl.ld.init(tl.kp, tl.vp, wave, wave);
-  const KeyMask mask{lim, INT_MIN, 0, h};
+  // The masks wait for the rows' lengths, while the first tiles are on their way.
+  KeyMask mask{0, INT_MIN, 0, h};
+  auto masks = [&] {
+    mask.lim = !valid     ? -1
+               : a.causal ? sq + a.Lp + sequence_length(a.lengths, b, a.Skv) - a.Sq
+                          : 0x7fffffff;  // the last key the row sees
+    tl.full_lo = wave_min_int(valid ? mask.lim : 0x7fffffff);
+  };
   // The floor keeps a zero scale well defined (every visible key gets weight 1).
   roll_tiles<D, false>(tl, last - tl.first, mt * BM + wave * 32 < rows, Stages{sk0, sk1, sv0, sv1},
-                       fr, row, fmaxf(a.c_abs, 1e-30f), mask);
+                       fr, row, fmaxf(a.c_abs, 1e-30f), mask, masks);
   if (a.P == 1)
     store_row<D>(row, h, valid ? a.o + orow * D : nullptr);
   else
-    store_state<D>(row, h, valid, a.ws_m, a.ws_l, a.ws_acc,
-                   orow * a.P + (packed ? p : a.P1 + p));
+    store_state<D>(row, h, valid, a.ws_m, a.ws_l, a.ws_acc, orow * a.P + (packed ? p : a.P1 + p),
+                   false);
 }
 
 }  // namespace

@@ -53,8 +53,8 @@ struct SelectParams {
 };
 
 // Attention over selected blocks (matrix-core kernel). With P > 1 the workgroups of a
-// row tile share its blocks and store partial states, m, l [rows][P] (base-2 units)
-// and acc [rows][P][D]; with P = 1 they write o.
+// row tile share its blocks and store partial states, m, l [rows][P] and
+// acc [rows][P][D]; with P = 1 they write o.
 struct BlocksParams {
   const uint16_t* q;   // [B][Hq][Sq][D] bf16
   const uint16_t* k;   // [B][Hkv][Skv][D] bf16
@@ -65,6 +65,8 @@ struct BlocksParams {
   float* ws_m;
   float* ws_l;
   float* ws_acc;
+  unsigned* counters;  // not null: the last workgroup of a (sequence, kv head) to store
+                       // its state combines (one row tile; see group_combine.hpp)
   int B, Hq, Hkv, Sq, Skv, D;
   int G, R;      // Hq / Hkv, rows of a kv head (G * Sq)
   int NB, shift, K;
@@ -107,10 +109,10 @@ struct PrefixParams {
   uint32_t qflip;
 };
 
-// o[row] = sum_p 2^(m_p - M) acc_p / sum_p 2^(m_p - M) l_p in bf16, 0 where no state
+// o[row] = sum_p e^(m_p - M) acc_p / sum_p e^(m_p - M) l_p in bf16, 0 where no state
 // has a key (M = -inf).
 struct StateCombineParams {
-  const float* m;  // [rows][P], base-2 units
+  const float* m;  // [rows][P], natural-log units
   const float* l;
   const float* acc;  // [rows][P][D]; not read where m is -inf
   uint16_t* o;       // [rows][D] bf16

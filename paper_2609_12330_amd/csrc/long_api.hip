@@ -107,15 +107,18 @@ ef_status ef_block_select(const void* q, const void* summary, const int* lengths
 
 namespace {
 
-// m, l [rows][P] and acc [rows][P][D] of a workspace of partial states.
+// A workspace of partial states: the arrival counters (a region of fixed place and size,
+// as in every workspace of the library), then m, l [rows][P] and acc [rows][P][D].
 struct StateLayout {
-  size_t l_off, acc_off, bytes;
+  size_t m_off, l_off, acc_off, bytes;
 };
 
 StateLayout state_layout(long long rows, long long P, int D) {
   StateLayout w;
-  w.l_off = ef::ws_align256((size_t)(rows * P) * sizeof(float));
-  w.acc_off = 2 * w.l_off;
+  const size_t a = ef::ws_align256((size_t)(rows * P) * sizeof(float));
+  w.m_off = ef::kCounterRegionBytes;
+  w.l_off = w.m_off + a;
+  w.acc_off = w.l_off + a;
   w.bytes = w.acc_off + (size_t)(rows * P) * D * sizeof(float);
   return w;
 }
@@ -123,7 +126,7 @@ StateLayout state_layout(long long rows, long long P, int D) {
 template <class Params>
 void set_states(Params& a, const StateLayout& w, void* workspace) {
   char* ws = static_cast<char*>(workspace);
-  a.ws_m = reinterpret_cast<float*>(ws);
+  a.ws_m = reinterpret_cast<float*>(ws + w.m_off);
   a.ws_l = reinterpret_cast<float*>(ws + w.l_off);
   a.ws_acc = reinterpret_cast<float*>(ws + w.acc_off);
 }
@@ -146,18 +149,26 @@ constexpr long long kFillWgs = 512;
 
 // Launch shape of attention over selected blocks. The rows of a kv head are cut into
 // tiles of `bm`; where these are few, P workgroups share a tile's blocks.
+//
+// 128 rows share a staged tile between four waves where such tiles fill the chip
+// twice; otherwise 64 do, whose lists' union is shorter. 64 / 128 rows (us; 16 blocks
+// of 512, 32/8 heads of 128; lists of neighbours alike, then independent): 4096 queries
+// 180 / 131, 2048 [512 workgroups of 128] 89 / 69 and 479 / 580, 1024 [256] 46.6 / 45.0
+// and 251 / 378, 512 38.8 / 38.6 and 138 / 200.
 struct BlocksPlan {
   int bm, mtiles, P;
+  bool fused;
 };
 
 BlocksPlan blocks_plan(const Shape& s, int nb, int topk) {
   BlocksPlan p;
   const long long R = (long long)(s.Hq / s.Hkv) * s.Sq;
-  p.bm = 64;
+  p.bm = (long long)s.B * s.Hkv * (R / 128) >= kFillWgs ? 128 : 64;
   p.mtiles = (int)((R + p.bm - 1) / p.bm);
   const long long groups = (long long)s.B * s.Hkv * p.mtiles;
   const long long most = std::max(1, std::min(std::min(nb, topk), 64));
   p.P = (int)std::min(std::max(kFillWgs / std::max(groups, 1LL), 1LL), most);
+  p.fused = p.mtiles == 1 && R * p.P <= 256 && (long long)s.B * s.Hkv <= ef::kCounterSlots;
   return p;
 }
 
@@ -176,7 +187,7 @@ struct PrefixPlan {
   long long n_prefix, n_own;
 };
 
-constexpr int kPrefixRows = 128;
+constexpr int kPrefixRows = 128;  // rows per workgroup
 
 // `tiles` tiles in about `parts` parts of at least `least` tiles: tiles per part.
 int tiles_per_part(long long tiles, long long parts, int least) {
@@ -196,8 +207,16 @@ PrefixPlan prefix_plan(const Shape& s, int Lp) {
     p.n_own = heads * p.mt2;
     return p;
   }
+  // Workgroups of the prefix: one to a compute unit keeps the matrix cores busy; half as
+  // many where the own keys have most of the work, which then get three of four places.
+  // 256 / 128 workgroups (us; 32/8 heads of 128, own keys half of the capacity in the
+  // mean; the prefix's part of the tiles in brackets): 64 sequences, 32768 + 2048 keys
+  // [0.33] 106 / 98, 16384 + 1024 [0.33] 57.7 / 54.9, 32 of them [0.33] 41 / 35, 16 [0.5]
+  // 27.2 / 28.0, 8 [0.67] 19.6 / 26.1, 64 over 32768 + 64 [0.94] 52 / 83.
+  const long long w1 = np * s.Hkv * p.mt1, w2 = no * heads * p.mt2;
+  const long long n1 = kFillWgs / (5 * w1 >= 3 * (w1 + w2) ? 2 : 4);
   if (np > 0) {
-    p.T1 = tiles_per_part(np, kFillWgs / 2 / (s.Hkv * (long long)p.mt1), 2);
+    p.T1 = tiles_per_part(np, n1 / (s.Hkv * (long long)p.mt1), 2);
     p.P1 = (int)((np + p.T1 - 1) / p.T1);
     p.n_prefix = (long long)s.Hkv * p.mt1 * p.P1;
   }
@@ -249,6 +268,8 @@ ef_status ef_attention_blocks(const void* q, const void* k, const void* v, const
     if (workspace == nullptr || workspace_bytes < w.bytes) return EF_ERR_WORKSPACE_TOO_SMALL;
     if (misaligned(workspace)) return EF_ERR_MISALIGNED;
     set_states(a, w, workspace);
+    // Few states: the last workgroup to store one combines its head's rows, in one launch.
+    a.counters = p.fused ? static_cast<unsigned*>(workspace) : nullptr;
   }
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k);
@@ -270,7 +291,7 @@ ef_status ef_attention_blocks(const void* q, const void* k, const void* v, const
   if ((long long)B * Hkv * p.mtiles * p.P >= (1LL << 31)) return EF_ERR_INVALID_SHAPE;
   hipStream_t hs = static_cast<hipStream_t>(stream);
   st = from_hip(ef::launch_attention_blocks(a, hs));
-  return st != EF_OK || p.P == 1 ? st : combine_states(a, s.rows(), hs);
+  return st != EF_OK || p.P == 1 || p.fused ? st : combine_states(a, s.rows(), hs);
 }
 
 size_t ef_attention_shared_prefix_workspace_size(int B, int Hq, int Hkv, int Sq, int Lp, int Skv,

@@ -4,6 +4,7 @@
 #pragma once
 
 #include "ef_long.hpp"
+#include "group_combine.hpp"
 #include "rolling.hpp"
 
 namespace ef {
@@ -61,11 +62,13 @@ struct Stages {
 // (at), loads it into a stage (load) and, with SEL, says whether this lane's row
 // sees it (on). A wave without rows (`active` false) only loads. Every wave of the
 // workgroup makes the call with the same n. The list's last tile may end in its
-// first half; any other tile may be ragged.
-template <int D, bool SEL, class Tiles>
+// first half; any other tile may be ragged. What `mask` and the tiles say of masks need
+// not be there before `ready` is called, behind the first loads.
+template <int D, bool SEL, class Tiles, class Ready>
 __device__ __forceinline__ void roll_tiles(const Tiles& tiles, int n, bool active,
                                            const Stages& st, const FragmentReads<D>& fr,
-                                           Rows<D>& rows, float c, const KeyMask& mask) {
+                                           Rows<D>& rows, float c, const KeyMask& mask,
+                                           Ready ready) {
   if (n <= 0) return;
   constexpr int SUB = TileGeom<D>::SUB;
   Rolling<D, SEL> ro{fr.k, fr.v, rows.qf, rows.oacc, rows.lsum, rows.mref, c};
@@ -80,6 +83,9 @@ __device__ __forceinline__ void roll_tiles(const Tiles& tiles, int n, bool activ
   tiles.template load<true>(st.k0, t0);
   tiles.template load<false>(st.v0, t0);
   tiles.template load<true>(st.k1, t1);
+  ready();
+  t0 = tile(0);
+  t1 = tile(1);
   wait_tile_loads();
   __syncthreads();
   if (active) {
@@ -142,25 +148,127 @@ __device__ __forceinline__ void store_row(const Rows<D>& rows, int h, uint16_t* 
       *reinterpret_cast<u32x2_t*>(orow + 32 * i + 8 * q + 4 * h) = w;
     }
 }
+// With `shared` the state is read by another workgroup of the launch: device-scope
+// stores (see group_combine.hpp).
 template <int D>
 __device__ __forceinline__ void store_state(const Rows<D>& rows, int h, bool valid, float* m,
-                                            float* l, float* acc, size_t slot) {
+                                            float* l, float* acc, size_t slot, bool shared) {
   const float lt = rows.lsum + __shfl_xor(rows.lsum, 32, 64);
   if (!valid) return;
   const bool none = rows.mref == kNoRef;
+  const float mref = none ? kNegInf : rows.mref * kLn2;  // natural-log units
+  if (shared) {
+    if (h == 0) {
+      store_dev(m + slot, mref);
+      store_dev(l + slot, lt);
+    }
+    if (none) return;
+    // (Shared states are few: their offsets fit 32 bits.)
+    const __amdgpu_buffer_rsrc_t rs =
+        __builtin_amdgcn_make_buffer_rsrc(acc, (short)0, -1, 0x00020000);
+    const unsigned off = ((unsigned)slot * D + 4 * h) * 4u;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const floatx16& x = rows.oacc[i];
+        const floatx4 v = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), rs,
+                                               (int)(off + (32 * i + 8 * q) * 4), 0,
+                                               16 /* device scope */);
+      }
+    return;
+  }
   if (h == 0) {
-    m[slot] = none ? kNegInf : rows.mref;
+    m[slot] = mref;
     l[slot] = lt;
   }
   if (none) return;
+  float* const row = acc + slot * D + 4 * h;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const floatx16& x = rows.oacc[i];
-      *reinterpret_cast<float4*>(acc + slot * D + 32 * i + 8 * q + 4 * h) =
+      *reinterpret_cast<float4*>(row + 32 * i + 8 * q) =
           make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
     }
+}
+
+// Combine, by the workgroup that stored the last of them, of the P states of rows row0
+// .. row0 + nrows - 1 into bf16 rows: what state_combine.hip does, on device-scope
+// loads. D / 4 lanes take a row, four channels each; P <= kFusedMaxP.
+template <int D, int NT>
+__device__ __forceinline__ void combine_shared(const float* m, const float* l, const float* acc,
+                                               uint16_t* o, size_t row0, int nrows, int P) {
+  constexpr int LPR = D / 4;              // lanes per row
+  constexpr int PPL = kFusedMaxP / LPR;   // states whose weights a lane forms
+  constexpr int BATCH = 8;                // value states in flight
+  const int ch = threadIdx.x % LPR;
+  // Rows are taken in whole waves: the lanes of a wave shuffle together.
+  for (int r0 = 0; r0 < nrows; r0 += NT / LPR) {
+    const int r = r0 + (int)threadIdx.x / LPR;
+    const bool valid = r < nrows;
+    const size_t base = (row0 + (valid ? r : 0)) * P;
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<float*>(acc + row0 * P * D), (short)0, nrows * P * D * 4, 0x00020000);
+    const int off = ((valid ? r : 0) * P * D + 4 * ch) * 4;
+    float mv[PPL], lv[PPL];
+#pragma unroll
+    for (int i = 0; i < PPL; ++i) {
+      const int p = ch + i * LPR;
+      mv[i] = p < P ? load_dev(m + base + p) : kNegInf;
+      lv[i] = p < P ? load_dev(l + base + p) : 0.f;
+    }
+    u32x4_t y[BATCH];
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) y[j] = load16_dev(rs, off + min(j, P - 1) * D * 4);
+    float M = mv[0];
+#pragma unroll
+    for (int i = 1; i < PPL; ++i) M = fmaxf(M, mv[i]);
+#pragma unroll
+    for (int x = 1; x < LPR; x *= 2) M = fmaxf(M, shfl_xor(M, x));
+    const float ref = M == kNegInf ? 0.f : M;
+    float L = 0.f;
+#pragma unroll
+    for (int i = 0; i < PPL; ++i) {
+      mv[i] = exp2_fast((mv[i] - ref) * kLog2e);  // 0 where the state has no key
+      L = fmaf(mv[i], lv[i], L);
+    }
+#pragma unroll
+    for (int x = 1; x < LPR; x *= 2) L += shfl_xor(L, x);
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = 0; p0 < P; p0 += BATCH) {
+      if (p0 > 0) {
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) y[j] = load16_dev(rs, off + min(p0 + j, P - 1) * D * 4);
+      }
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        const int p = p0 + j;
+        float w = 0.f;
+#pragma unroll
+        for (int i = 0; i < PPL; ++i) {
+          const float x = __shfl(mv[i], p % LPR, LPR);
+          w = p / LPR == i ? x : w;
+        }
+        w = p < P ? w : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)  // (a state without a key was not stored)
+          s[e] = w > 0.f ? fmaf(w, __uint_as_float(y[j][e]), s[e]) : s[e];
+      }
+    }
+    const float inv = L > 0.f ? 1.f / L : 0.f;
+    const u32x2_t w = {pack_bf16x2(s[0] * inv, s[1] * inv), pack_bf16x2(s[2] * inv, s[3] * inv)};
+    if (valid) *reinterpret_cast<u32x2_t*>(o + (row0 + r) * D + 4 * ch) = w;
+  }
+}
+
+// The output rows made visibly invalid, where the arrivals cannot be trusted (a counter
+// that was not zero when the launch began).
+template <int D, int NT>
+__device__ __forceinline__ void poison_rows(uint16_t* o, size_t row0, int nrows) {
+  for (int i = threadIdx.x; i < nrows * D; i += NT) o[row0 * D + i] = 0x7fc0;
 }
 
 }  // namespace ef

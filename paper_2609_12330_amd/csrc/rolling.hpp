@@ -411,20 +411,20 @@ struct StageLoader {
       koff[i] = row0 * G::ROW + (slot ^ G::swz_k(row0 + i * G::RPI)) * 16;
     voff = vrow0 * G::ROW + (slot ^ G::swz_v(vrow0)) * 16;
   }
-  // Block I of a whole tile.
-  template <bool ISK, int I>
+  // Block I of a whole tile. AUX: cache policy of the load (2: non-temporal).
+  template <bool ISK, int I, int AUX>
   __device__ __forceinline__ void block(char* l, unsigned soff) const {
     constexpr int hi = I / 4 * 4096;  // past the 12-bit instruction offset
     if constexpr (ISK)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           krs, (__attribute__((address_space(3))) void*)(l + hi), 16, (int)koff[I % NK],
-          (int)(soff + hi), I % 4 * 1024, 0);
+          (int)(soff + hi), I % 4 * 1024, AUX);
     else
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           vrs, (__attribute__((address_space(3))) void*)(l + hi), 16, (int)voff,
-          (int)(soff + hi), I % 4 * 1024, 0);
+          (int)(soff + hi), I % 4 * 1024, AUX);
   }
-  template <bool ISK>
+  template <bool ISK, int AUX = 0>
   __device__ __forceinline__ void load(char* stage, int kb, int kend) const {
     const int nrows = kend - kb;
     if (nrows <= 0) return;  // a tile past the last one
@@ -432,7 +432,7 @@ struct StageLoader {
     char* l = stage + (ISK ? wbase : vwbase);
     const unsigned soff = (unsigned)kb * G::ROW;
     if (nrows >= 64) {
-      static_for<N>([&](auto q) { block<ISK, decltype(q)::value>(l, soff); });
+      static_for<N>([&](auto q) { block<ISK, decltype(q)::value, AUX>(l, soff); });
     } else {
       // Ragged tile: rows past the run repeat its last row (masked later).
 #pragma unroll
@@ -442,9 +442,9 @@ struct StageLoader {
         const int off = min(r, nrows - 1) * G::ROW + c * 16;
         auto* d = (__attribute__((address_space(3))) void*)(l + i * 1024);
         if constexpr (ISK)
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(krs, d, 16, off, (int)soff, 0, 0);
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(krs, d, 16, off, (int)soff, 0, AUX);
         else
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(vrs, d, 16, off, (int)soff, 0, 0);
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(vrs, d, 16, off, (int)soff, 0, AUX);
       }
     }
   }

@@ -1,5 +1,5 @@
 // Combine of stored partial states into bf16 rows: with M = max m_p,
-//   o = sum_p 2^(m_p - M) acc_p / sum_p 2^(m_p - M) l_p   (0 where every m_p is -inf),
+//   o = sum_p e^(m_p - M) acc_p / sum_p e^(m_p - M) l_p   (0 where every m_p is -inf),
 // the sums in fp32, one rounding to bf16 at the end.
 //
 // One wave per row: the lanes first form the weights of up to 64 states at a time
@@ -34,8 +34,8 @@ __global__ __launch_bounds__(kCombineWaves * 64) void state_combine_kernel(State
 #pragma unroll
     for (int off = 1; off < 64; off *= 2) top = fmaxf(top, shfl_xor(top, off));
     const float ref = top == kNegInf ? 0.f : top;
-    const float w = exp2_fast(m - ref);  // 0 where m = -inf
-    const float old = exp2_fast(M - ref);
+    const float w = exp2_fast((m - ref) * kLog2e);  // 0 where m = -inf
+    const float old = exp2_fast((M - ref) * kLog2e);
     float sum = w > 0.f ? w * l : 0.f;
 #pragma unroll
     for (int off = 1; off < 64; off *= 2) sum += shfl_xor(sum, off);

@@ -750,13 +750,23 @@ def _out_bf16(q, out):
     return out
 
 
+def _state_workspace(n, q):
+    """n bytes on q's device, the arrival counters at their start zero (they stay zero from call
+    to call); None for 0 bytes."""
+    if n == 0:
+        return None
+    workspace = _torch().empty(n, dtype=_torch().uint8, device=q.device)
+    workspace[:COUNTER_REGION_BYTES].zero_()
+    return workspace
+
+
 def _own_workspace(workspace, size, sizes, q):
     """(pointer, bytes, tensor) of the workspace given, or of a new one of size(*sizes) bytes."""
     if workspace is None:
         n = size(*sizes)
         if n == 0:
             return None, 0, None
-        workspace = _torch().empty(n, dtype=_torch().uint8, device=q.device)
+        workspace = _state_workspace(n, q)
     if workspace.get_device() != q.get_device() or not workspace.is_contiguous():
         _check_workspace(workspace, q)
     return workspace.data_ptr(), workspace.nbytes, workspace
@@ -767,7 +777,7 @@ def make_blocks_workspace(q, k, topk: int, block_size: int = 64):
     B, Hq, Sq, D = q.shape
     n = int(ef_attention_blocks_workspace_size(B, Hq, k.shape[1], Sq, k.shape[2], D, block_size,
                                                topk))
-    return _torch().empty(n, dtype=_torch().uint8, device=q.device) if n else None
+    return _state_workspace(n, q)
 
 
 def attention_blocks(q, k, v, blocks, block_size: int = 64, scale: Optional[float] = None,
@@ -800,7 +810,7 @@ def make_shared_prefix_workspace(q, k_prefix, k):
     B, Hq, Sq, D = q.shape
     n = int(ef_attention_shared_prefix_workspace_size(B, Hq, k.shape[1], Sq, k_prefix.shape[1],
                                                       k.shape[2], D))
-    return _torch().empty(n, dtype=_torch().uint8, device=q.device) if n else None
+    return _state_workspace(n, q)
 
 
 def attention_shared_prefix(q, k_prefix, v_prefix, k, v, scale: Optional[float] = None,
