@@ -23,9 +23,9 @@
 // their smallest and largest finds, each step one ballot (a somewhat lower bound does,
 // so it stops early). The few scores above that bound less 2 E then go one to a lane,
 // in index order, for a second bisection. They hold every block within 2 E of the
-// border too. Where that does not apply (need > 64, or more than 64
-// such scores, as where many are equal) a bisection over order-preserving integers counts all
-// scores, and a border of any length is settled in LDS.
+// border too. Where that does not apply (need > 64, or more than 64 such scores) the
+// second bisection counts all scores; a border of more than 64 (many equal scores) is
+// settled in LDS.
 #include "ef_long.hpp"
 #include "ef_device.hpp"
 
@@ -36,8 +36,8 @@ namespace ef {
 namespace {
 
 // LDS pointers by type: through plain ones the compiler loses sight of the address space
-// and reads LDS with flat loads, which wait for each other (choice of a position 5.6
-// -> ?).
+// and reads LDS with flat loads, which wait for each other (4096 queries of 1024 blocks
+// 150 -> 130 us).
 typedef __attribute__((address_space(3))) float lds_float;
 typedef __attribute__((address_space(3))) unsigned long long lds_u64;
 typedef __attribute__((address_space(3))) u32x4_t lds_chunk;
@@ -245,6 +245,26 @@ struct Keys {
   }
 };
 
+// A T in [lo, hi] with count(T) = need, or the largest with count(T) >= need, by halves of
+// the interval of values, a step per bit of the answer's place among them (halving the
+// integers would first look for its exponent), then of the integers between. On entry
+// count(lo) = cnt >= need and nothing is above hi.
+template <class F>
+__device__ __forceinline__ uint32_t bisect(uint32_t lo, uint32_t hi, int need, int& cnt, F count) {
+  for (int step = 0; cnt != need && lo < hi; ++step) {
+    uint32_t mid = ordered(0.5f * unordered(lo) + 0.5f * unordered(hi));
+    if (step >= 16 || mid <= lo || mid > hi) mid = hi - (hi - lo) / 2;
+    const int n = count(mid);
+    if (n >= need) {
+      lo = mid;
+      cnt = n;
+    } else {
+      hi = mid - 1;
+    }
+  }
+  return lo;
+}
+
 // One position's choice among the blocks [c0, c1), which are more than the `need` wanted
 // ones, by one wave. sc: the scores (NaN where every head's product was); bound: their
 // largest error.
@@ -264,12 +284,33 @@ struct Choice {
   __device__ __forceinline__ float apart(float x) const {
     return 2.f * bound + (fabsf(x) < -kNegInf ? 4.8e-7f * fabsf(x) : 0.f) + 1e-30f;
   }
+
+  // Among the lanes of the set, each with a block, in ascending order: how many come
+  // before this one's by exact score, then index.
+  template <int D>
+  __device__ __forceinline__ int exact_rank(unsigned long long set, int block) const {
+    const int lane = threadIdx.x & 63;
+    double exact = 0.0;
+    for (unsigned long long m = set; m; m &= m - 1) {
+      const int j = __builtin_ctzll(m);
+      const int n = __builtin_amdgcn_readlane(block, j);
+      const double e = exact_score<D>(q, head_stride, G, s + (size_t)n * D);
+      if (lane == j) exact = e;
+    }
+    int rank = 0;
+    for (unsigned long long m = set; m; m &= m - 1) {
+      const int j = __builtin_ctzll(m);
+      const double e = __shfl(exact, j, 64);
+      rank += e > exact || (e == exact && j < lane) ? 1 : 0;
+    }
+    return rank;
+  }
 };
 
-// The choice where few scores come into question; false, with nothing written, where
-// they are not few. scratch: 65 words of LDS.
+// The choice by fp32 scores, and by exact ones where few scores come into question; false,
+// with nothing written, where exact scores of more than 64 blocks are called for. scratch: 65 words of LDS.
 template <int D, int NV>
-__device__ __forceinline__ bool choose_few(const Choice& a, lds_u64* scratch) {
+__device__ __forceinline__ bool choose(const Choice& a, lds_u64* scratch) {
   const int lane = threadIdx.x & 63;
   const int c0 = a.c0, c1 = a.c1, need = a.need;
   Keys<NV> keys{a.sc, c0, c1, {}};
@@ -284,12 +325,10 @@ __device__ __forceinline__ bool choose_few(const Choice& a, lds_u64* scratch) {
     few = keys.fetch(0);
     few_block = c0 + lane;
   } else if (need <= 64) {
-    // Halving the interval of values takes a step per bit of the answer's place among
-    // them; the integers' would first look for its exponent.
     const float best = unordered(mine);
     float least = unordered(__builtin_amdgcn_readfirstlane(wave_min(mine)));
     float hi = unordered(top);
-    for (int k = 64, most = need + (64 - need) / 4, step = 0; k > most && step < 16; ++step) {
+    for (int k = 64, most = need + (64 - need) / 8, step = 0; k > most && step < 16; ++step) {
       const float mid = 0.5f * least + 0.5f * hi;
       const int n = (int)__popcll(__ballot(best >= mid));
       if (n >= need && mid > least) {
@@ -323,22 +362,10 @@ __device__ __forceinline__ bool choose_few(const Choice& a, lds_u64* scratch) {
     wave_lds_sync();  // read before the wave's next position writes
   }
   if (held <= 64) {
-    // A T with just `need` of the few at or above it, or the largest with at least that
-    // many: by halves of the interval of values, then of the integers between.
-    uint32_t T = __builtin_amdgcn_readfirstlane(wave_min(lane < held ? few : 0xffffffffu));
-    uint32_t hi = top;
     int cnt = held;
-    for (int step = 0; cnt != need && T < hi; ++step) {
-      uint32_t mid = ordered(0.5f * unordered(T) + 0.5f * unordered(hi));
-      if (step >= 16 || mid <= T || mid > hi) mid = hi - (hi - T) / 2;
-      const int n = (int)__popcll(__ballot(few >= mid));
-      if (n >= need) {
-        T = mid;
-        cnt = n;
-      } else {
-        hi = mid - 1;
-      }
-    }
+    const uint32_t T =
+        bisect(__builtin_amdgcn_readfirstlane(wave_min(lane < held ? few : 0xffffffffu)), top,
+               need, cnt, [&](uint32_t t) { return (int)__popcll(__ballot(few >= t)); });
     bool take = few >= T;
     // Last score in, first one out (where that is none of the few, more than e2 below).
     const float least = unordered(wave_min(take ? few : 0xffffffffu));
@@ -352,29 +379,63 @@ __device__ __forceinline__ bool choose_few(const Choice& a, lds_u64* scratch) {
       const bool near = few != 0 && !sure && (!finite || x >= least - e2);
       const unsigned long long todo = __ballot(near);
       const int want = need - (int)__popcll(__ballot(sure));
-      double exact = 0.0;
-      for (unsigned long long m = todo; m; m &= m - 1) {
-        const int j = __builtin_ctzll(m);
-        const int n = __builtin_amdgcn_readlane(few_block, j);
-        const double e = exact_score<D>(a.q, a.head_stride, a.G, a.s + (size_t)n * D);
-        if (lane == j) exact = e;
-      }
-      int rank = 0;  // blocks near the border that come before this lane's
-      for (unsigned long long m = todo; m; m &= m - 1) {
-        const int j = __builtin_ctzll(m);
-        const double e = __shfl(exact, j, 64);
-        rank += e > exact || (e == exact && j < lane) ? 1 : 0;
-      }
+      const int rank = a.template exact_rank<D>(todo, few_block);
       take = sure || (near && rank < want);
     }
     const int slot = (int)__popcll(__ballot(take) & ((1ull << lane) - 1));
     if (take && slot < need) a.out[slot] = few_block;
     return true;
   }
-  return false;
+
+  // Too many for the lanes: the same on all scores, unless exact ones are called for.
+  int cnt = c1 - c0;
+  const uint32_t T = bisect(0, top, need, cnt, [&](uint32_t t) { return keys.count(t); });
+  uint32_t in = 0xffffffffu, outside = 0;
+  keys.each([&](int, uint32_t x) {
+    in = min(in, x >= T ? x : 0xffffffffu);
+    outside = max(outside, x >= T ? 0u : x);
+  });
+  const float least = unordered(wave_min(in));
+  const float e2 = a.apart(least);
+  uint32_t first = T, sure = T;  // scores from `sure` on are in, from `first` on perhaps
+  unsigned long long chosen = 0;  // which of the latter, in index order
+  if (cnt != need || !(least - unordered(wave_max(outside)) > e2)) {
+    const bool finite = e2 < -kNegInf && least > kNegInf;
+    if (!finite) return false;
+    first = ordered(least - e2);
+    sure = ordered(least + e2) + 1;
+    const int want = need - keys.count(sure);
+    int near = 0;
+    keys.each([&](int i, uint32_t x) {
+      const bool at = x >= first && x < sure;
+      const unsigned long long m = __ballot(at);
+      const int slot = near + (int)__popcll(m & ((1ull << lane) - 1));
+      scratch[at ? min(slot, 64) : 64] = (uint32_t)(c0 + 64 * i + lane);
+      near += (int)__popcll(m);
+    });
+    if (near > 64) return false;
+    wave_lds_sync();
+    const int block = lane < near ? (int)scratch[lane] : 0;
+    wave_lds_sync();
+    const unsigned long long set = near < 64 ? (1ull << near) - 1 : ~0ull;
+    const int rank = a.template exact_rank<D>(set, block);
+    chosen = __ballot(lane < near && rank < want);
+  }
+  int at = 0, seen = 0;
+  keys.each([&](int i, uint32_t x) {
+    const unsigned long long m = __ballot(x >= first && x < sure);
+    const int j = seen + (int)__popcll(m & ((1ull << lane) - 1));
+    const bool take = x >= sure || (x >= first && j < 64 && (chosen >> j & 1));
+    const unsigned long long t = __ballot(take);
+    const int slot = at + (int)__popcll(t & ((1ull << lane) - 1));
+    if (take && slot < need) a.out[slot] = c0 + 64 * i + lane;
+    at += (int)__popcll(t);
+    seen += (int)__popcll(m);
+  });
+  return true;
 }
 
-// The choice where many scores are equal or many blocks wanted.
+// The choice where more than 64 scores may be at the border.
 template <int D>
 __device__ __forceinline__ void choose_many(const Choice& a) {
   const int lane = threadIdx.x & 63;
@@ -385,17 +446,7 @@ __device__ __forceinline__ void choose_many(const Choice& a) {
   keys.each([&](int, uint32_t x) { top = max(top, x); });
   top = __builtin_amdgcn_readfirstlane(wave_max(top));
   int cnt = c1 - c0;
-  uint32_t T = 0;
-  for (uint32_t hi = top; cnt != need && T < hi;) {
-    const uint32_t mid = hi - (hi - T) / 2;
-    const int n = keys.count(mid);
-    if (n >= need) {
-      T = mid;
-      cnt = n;
-    } else {
-      hi = mid - 1;
-    }
-  }
+  uint32_t T = bisect(0, top, need, cnt, [&](uint32_t t) { return keys.count(t); });
   uint32_t in = 0xffffffffu, outside = 0;
   keys.each([&](int, uint32_t x) {
     in = min(in, x >= T ? x : 0xffffffffu);
@@ -659,9 +710,9 @@ void block_select_kernel(SelectParams a) {
     for (int i = c1 + lane; i <= cur; i += 64) out[a.K - 1 - (cur - i)] = i;
     if (ch.need == 0) continue;
     lds_u64* const words = (lds_u64*)scratch[wave];
-    const bool done = c1 - c0 <= 64 * 4    ? choose_few<D, 4>(ch, words)
-                      : c1 - c0 <= 64 * 16 ? choose_few<D, 16>(ch, words)
-                                           : choose_few<D, 0>(ch, words);
+    const bool done = c1 - c0 <= 64 * 4    ? choose<D, 4>(ch, words)
+                      : c1 - c0 <= 64 * 16 ? choose<D, 16>(ch, words)
+                                           : choose<D, 0>(ch, words);
     if (!done) choose_many<D>(ch);
   }
 }

@@ -188,3 +188,23 @@ def test_oracle_attention_agrees_with_the_plain_one():
     short = oracle.shared_prefix_ref(q, kp, vp, k, v, 0.2, True, [30, 2])
     assert np.allclose(short[0], oracle.attention_ref(q[:1], kk[:1, :, :49], vv[:1, :, :49], 0.2,
                                                       True)[0], atol=1e-12)
+
+
+def test_tensors_that_are_refused():
+    """The torch-level calls check their tensors before the library sees them."""
+    import torch
+    bf = torch.bfloat16
+    q, k = torch.zeros(1, 4, 2, 64, dtype=bf), torch.zeros(1, 2, 100, 64, dtype=bf)
+    lists = torch.zeros(1, 2, 2, 3, dtype=torch.int32)
+    m = torch.zeros(1, 2, 2, 64, dtype=bf)
+    kp = torch.zeros(2, 30, 64, dtype=bf)
+    for call in (lambda: ef.block_summary(k), lambda: ef.block_select(q, m, 100, 3),
+                 lambda: ef.attention_blocks(q, k, k, lists),
+                 lambda: ef.attention_shared_prefix(q, kp, kp, k, k)):
+        with pytest.raises(TypeError, match="GPU"):
+            call()
+    for call in (lambda: ef.block_summary(k.float()), lambda: ef.block_select(q.half(), m, 100, 3),
+                 lambda: ef.attention_blocks(q.float(), k, k, lists),
+                 lambda: ef.attention_shared_prefix(q.float(), kp, kp, k, k)):
+        with pytest.raises(TypeError, match="bfloat16"):
+            call()

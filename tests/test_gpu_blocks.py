@@ -264,3 +264,40 @@ def test_all_blocks_is_plain_causal_attention():
     torch.cuda.synchronize()
     # Both round the weights: twice the tolerance of one.
     close(got, f64(ref), 2 * f64(mag), "plain")
+
+
+def test_refused_tensors():
+    """Shapes, types and strides that do not fit are refused before anything is enqueued."""
+    announce("refused tensors")
+    bf = torch.bfloat16
+    q, k = (torch.zeros(1, h, n, 64, dtype=bf, device="cuda") for h, n in ((4, 2), (2, 100)))
+    lists = torch.zeros(1, 2, 2, 3, dtype=torch.int32, device="cuda")
+    m = torch.zeros(1, 2, 2, 64, dtype=bf, device="cuda")
+    kp = torch.zeros(2, 30, 64, dtype=bf, device="cuda")
+    n = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for exc, call in (
+            (ValueError, lambda: ef.block_summary(k.transpose(1, 2))),
+            (ValueError, lambda: ef.block_summary(k, 32)),
+            (ValueError, lambda: ef.block_summary(k, new_keys=1)),
+            (ValueError, lambda: ef.block_summary(k, out=m[:, :1].contiguous())),
+            (TypeError, lambda: ef.block_summary(k, lengths=n.long())),
+            (ValueError, lambda: ef.block_summary(k, lengths=n.repeat(2))),
+            (TypeError, lambda: ef.block_summary(k, lengths=n.cpu())),
+            (ef.EfError, lambda: ef.block_summary(k, new_keys=-1, out=m)),
+            (ValueError, lambda: ef.block_select(q, m, 200, 3)),
+            (ef.EfError, lambda: ef.block_select(q, m, 100, 1, sink_blocks=1)),
+            (ef.EfError, lambda: ef.block_select(q, m, 100, 257)),
+            (TypeError, lambda: ef.block_select(q, m, 100, 3, out=lists.long())),
+            (TypeError, lambda: ef.attention_blocks(q, k, k, lists.long())),
+            (ValueError, lambda: ef.attention_blocks(q, k, k, lists[:, :, :1].contiguous())),
+            (ValueError, lambda: ef.attention_blocks(q, k, k[:, :, :50].contiguous(), lists)),
+            (TypeError, lambda: ef.attention_blocks(q, k, k, lists, out=q.float())),
+            (ef.EfError, lambda: ef.attention_blocks(q, k, k, lists, block_size=96)),
+            (ef.EfError, lambda: ef.attention_blocks(q, k, k, lists, scale=float("nan"))),
+            (ef.EfError, lambda: ef.attention_blocks(q, k, k, lists, workspace=n.byte())),
+            (ValueError, lambda: ef.attention_shared_prefix(q, kp[:1].contiguous(), kp, k, k)),
+            (ValueError, lambda: ef.attention_shared_prefix(q, kp, kp[:, :9].contiguous(), k, k)),
+            (ef.EfError, lambda: ef.attention_shared_prefix(q, kp, kp, k, k, workspace=n))):
+        with pytest.raises(exc):
+            call()
+    torch.cuda.synchronize()
