@@ -39,7 +39,7 @@ namespace {
 // and reads LDS with flat loads, which wait for each other (4096 queries of 1024 blocks
 // 150 -> 130 us).
 typedef __attribute__((address_space(3))) float lds_float;
-typedef __attribute__((address_space(3))) unsigned long long lds_u64;
+typedef __attribute__((address_space(3))) int lds_int;
 typedef __attribute__((address_space(3))) u32x4_t lds_chunk;
 
 // Order-preserving integer of a float (no NaN).
@@ -212,38 +212,52 @@ __device__ __forceinline__ void settle_border(lds_float* sc, int c0, int c1, flo
   wave_lds_sync();
 }
 
-// The scores of the blocks [c0, c1) of one position as integers, every 64th in a
-// lane's registers; with NV = 0 (more than 64 a lane) they stay in LDS.
+// The scores of the blocks [c0, c1) of one position, every 64th in a lane's registers;
+// with NV = 0 (more than 64 a lane) they stay in LDS.
 template <int NV>
-struct Keys {
+struct Scores {
   const lds_float* sc;
   int c0, c1;
-  uint32_t u[NV > 0 ? NV : 1];
-  __device__ __forceinline__ uint32_t fetch(int i) const {  // 0: no block; NaN is -inf
-    const int n = c0 + 64 * i + (threadIdx.x & 63);
+  float v[NV > 0 ? NV : 1];
+  __device__ __forceinline__ bool has(int i) const {
+    return c0 + 64 * i + (int)(threadIdx.x & 63) < c1;
+  }
+  __device__ __forceinline__ float fetch(int i) const {  // -inf: no block
+    const int n = c0 + 64 * i + (int)(threadIdx.x & 63);
     const float x = sc[min(n, c1 - 1)];
-    return n < c1 ? ordered(x == x ? x : kNegInf) : 0u;
+    return n < c1 ? x : kNegInf;
   }
   __device__ __forceinline__ void load() {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) u[i] = fetch(i);
+    for (int i = 0; i < NV; ++i) v[i] = fetch(i);
   }
-  // f(i, key of block c0 + 64 i + lane), ascending in i, all lanes together.
+  // f(i, score of block c0 + 64 i + lane), ascending in i, all lanes together.
   template <class F>
   __device__ __forceinline__ void each(F f) const {
     if constexpr (NV > 0) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) f(i, u[i]);
+      for (int i = 0; i < NV; ++i) f(i, v[i]);
     } else {
       for (int i = 0; c0 + 64 * i < c1; ++i) f(i, fetch(i));
     }
   }
+  // The same with the score as an integer, 0 where there is no block.
+  template <class F>
+  __device__ __forceinline__ void each_key(F f) const {
+    each([&](int i, float x) { f(i, has(i) ? ordered(x) : 0u); });
+  }
   __device__ __forceinline__ int count(uint32_t least) const {
     int k = 0;
-    each([&](int, uint32_t x) { k += (int)__popcll(__ballot(x >= least)); });
+    each_key([&](int, uint32_t x) { k += (int)__popcll(__ballot(x >= least)); });
     return k;
   }
 };
+
+// Lanes of the set below this one, added to n.
+__device__ __forceinline__ int rank_in(unsigned long long set, int n = 0) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(set >> 32),
+                                        __builtin_amdgcn_mbcnt_lo((uint32_t)set, (uint32_t)n));
+}
 
 // A T in [lo, hi] with count(T) = need, or the largest with count(T) >= need, by halves of
 // the interval of values, a step per bit of the answer's place among them (halving the
@@ -266,7 +280,7 @@ __device__ __forceinline__ uint32_t bisect(uint32_t lo, uint32_t hi, int need, i
 }
 
 // One position's choice among the blocks [c0, c1), which are more than the `need` wanted
-// ones, by one wave. sc: the scores (NaN where every head's product was); bound: their
+// ones, by one wave. sc: the scores; bound: their
 // largest error.
 struct Choice {
   lds_float* sc;
@@ -310,24 +324,24 @@ struct Choice {
 // The choice by fp32 scores, and by exact ones where few scores come into question; false,
 // with nothing written, where exact scores of more than 64 blocks are called for. scratch: 65 words of LDS.
 template <int D, int NV>
-__device__ __forceinline__ bool choose(const Choice& a, lds_u64* scratch) {
+__device__ __forceinline__ bool choose(const Choice& a, lds_int* scratch) {
   const int lane = threadIdx.x & 63;
   const int c0 = a.c0, c1 = a.c1, need = a.need;
-  Keys<NV> keys{a.sc, c0, c1, {}};
-  keys.load();
-  uint32_t mine = 0;  // this lane's largest
-  keys.each([&](int, uint32_t x) { mine = max(mine, x); });
-  const uint32_t top = __builtin_amdgcn_readfirstlane(wave_max(mine));
+  Scores<NV> scores{a.sc, c0, c1, {}};
+  scores.load();
+  float best = kNegInf;  // this lane's largest
+  scores.each([&](int, float x) { best = fmaxf(best, x); });
+  const float most_of_all = __builtin_bit_cast(
+      float, __builtin_amdgcn_readfirstlane(__float_as_int(wave_max(best))));
+  const uint32_t top = ordered(most_of_all);
   // The few scores that can be in or near the border, one to a lane, in index order.
   uint32_t few = 0;
-  int few_block = 0, held = c1 - c0;
+  int few_block = c0 + lane, held = c1 - c0;
   if (held <= 64) {
-    few = keys.fetch(0);
-    few_block = c0 + lane;
+    few = scores.has(0) ? ordered(scores.fetch(0)) : 0u;
   } else if (need <= 64) {
-    const float best = unordered(mine);
-    float least = unordered(__builtin_amdgcn_readfirstlane(wave_min(mine)));
-    float hi = unordered(top);
+    float least = -wave_max(-best);
+    float hi = most_of_all;
     for (int k = 64, most = need + (64 - need) / 8, step = 0; k > most && step < 16; ++step) {
       const float mid = 0.5f * least + 0.5f * hi;
       const int n = (int)__popcll(__ballot(best >= mid));
@@ -338,27 +352,19 @@ __device__ __forceinline__ bool choose(const Choice& a, lds_u64* scratch) {
         hi = mid;  // (NaN with infinite ends: no further step changes anything)
       }
     }
-    const float margin = fmaxf(a.apart(least), a.apart(unordered(top)));
-    const uint32_t base = margin < -kNegInf && least > kNegInf ? ordered(least - margin) : 0u;
+    // (Minus an infinite bound this is -inf, or NaN: then they are not few.)
+    const float base = least - fmaxf(a.apart(least), a.apart(most_of_all));
     held = 0;
-    keys.each([&](int i, uint32_t x) {
+    scores.each([&](int i, float x) {
       const unsigned long long m = __ballot(x >= base);
-      const int slot = held + (int)__builtin_amdgcn_mbcnt_hi(
-                                  (uint32_t)(m >> 32),
-                                  __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
       // Word 64 takes what has no place.
-      scratch[x >= base ? min(slot, 64) : 64] =
-          (unsigned long long)x << 32 | (uint32_t)(c0 + 64 * i + lane);
+      scratch[x >= base ? min(rank_in(m, held), 64) : 64] = c0 + 64 * i + lane;
       held += (int)__popcll(m);
     });
-    if (held <= 64) {
-      wave_lds_sync();
-      const unsigned long long w = scratch[lane];
-      if (lane < held) {
-        few = (uint32_t)(w >> 32);
-        few_block = (int)(uint32_t)w;
-      }
-    }
+    if (!(base > kNegInf)) held = 65;
+    wave_lds_sync();
+    if (lane < held) few_block = scratch[lane];
+    if (lane < held && held <= 64) few = ordered(a.sc[few_block]);
     wave_lds_sync();  // read before the wave's next position writes
   }
   if (held <= 64) {
@@ -382,16 +388,16 @@ __device__ __forceinline__ bool choose(const Choice& a, lds_u64* scratch) {
       const int rank = a.template exact_rank<D>(todo, few_block);
       take = sure || (near && rank < want);
     }
-    const int slot = (int)__popcll(__ballot(take) & ((1ull << lane) - 1));
+    const int slot = rank_in(__ballot(take));
     if (take && slot < need) a.out[slot] = few_block;
     return true;
   }
 
   // Too many for the lanes: the same on all scores, unless exact ones are called for.
   int cnt = c1 - c0;
-  const uint32_t T = bisect(0, top, need, cnt, [&](uint32_t t) { return keys.count(t); });
+  const uint32_t T = bisect(0, top, need, cnt, [&](uint32_t t) { return scores.count(t); });
   uint32_t in = 0xffffffffu, outside = 0;
-  keys.each([&](int, uint32_t x) {
+  scores.each_key([&](int, uint32_t x) {
     in = min(in, x >= T ? x : 0xffffffffu);
     outside = max(outside, x >= T ? 0u : x);
   });
@@ -404,30 +410,30 @@ __device__ __forceinline__ bool choose(const Choice& a, lds_u64* scratch) {
     if (!finite) return false;
     first = ordered(least - e2);
     sure = ordered(least + e2) + 1;
-    const int want = need - keys.count(sure);
+    const int want = need - scores.count(sure);
     int near = 0;
-    keys.each([&](int i, uint32_t x) {
+    scores.each_key([&](int i, uint32_t x) {
       const bool at = x >= first && x < sure;
       const unsigned long long m = __ballot(at);
-      const int slot = near + (int)__popcll(m & ((1ull << lane) - 1));
-      scratch[at ? min(slot, 64) : 64] = (uint32_t)(c0 + 64 * i + lane);
+      const int slot = rank_in(m, near);
+      scratch[at ? min(slot, 64) : 64] = c0 + 64 * i + lane;
       near += (int)__popcll(m);
     });
     if (near > 64) return false;
     wave_lds_sync();
-    const int block = lane < near ? (int)scratch[lane] : 0;
+    const int block = lane < near ? scratch[lane] : 0;
     wave_lds_sync();
     const unsigned long long set = near < 64 ? (1ull << near) - 1 : ~0ull;
     const int rank = a.template exact_rank<D>(set, block);
     chosen = __ballot(lane < near && rank < want);
   }
   int at = 0, seen = 0;
-  keys.each([&](int i, uint32_t x) {
+  scores.each_key([&](int i, uint32_t x) {
     const unsigned long long m = __ballot(x >= first && x < sure);
-    const int j = seen + (int)__popcll(m & ((1ull << lane) - 1));
+    const int j = rank_in(m, seen);
     const bool take = x >= sure || (x >= first && j < 64 && (chosen >> j & 1));
     const unsigned long long t = __ballot(take);
-    const int slot = at + (int)__popcll(t & ((1ull << lane) - 1));
+    const int slot = rank_in(t, at);
     if (take && slot < need) a.out[slot] = c0 + 64 * i + lane;
     at += (int)__popcll(t);
     seen += (int)__popcll(m);
@@ -441,14 +447,14 @@ __device__ __forceinline__ void choose_many(const Choice& a) {
   const int lane = threadIdx.x & 63;
   const int c0 = a.c0, c1 = a.c1, need = a.need;
   lds_float* const sc = a.sc;
-  const Keys<0> keys{sc, c0, c1, {}};
+  const Scores<0> scores{sc, c0, c1, {}};
   uint32_t top = 0;
-  keys.each([&](int, uint32_t x) { top = max(top, x); });
+  scores.each_key([&](int, uint32_t x) { top = max(top, x); });
   top = __builtin_amdgcn_readfirstlane(wave_max(top));
   int cnt = c1 - c0;
-  uint32_t T = bisect(0, top, need, cnt, [&](uint32_t t) { return keys.count(t); });
+  uint32_t T = bisect(0, top, need, cnt, [&](uint32_t t) { return scores.count(t); });
   uint32_t in = 0xffffffffu, outside = 0;
-  keys.each([&](int, uint32_t x) {
+  scores.each_key([&](int, uint32_t x) {
     in = min(in, x >= T ? x : 0xffffffffu);
     outside = max(outside, x >= T ? 0u : x);
   });
@@ -456,9 +462,6 @@ __device__ __forceinline__ void choose_many(const Choice& a) {
   const float next = cnt != need ? least : unordered(wave_max(outside));
   const float e2 = a.apart(least);
   if (!(least - next > e2)) {
-    for (int n = c0 + lane; n < c1; n += 64)
-      if (sc[n] != sc[n]) sc[n] = kNegInf;
-    wave_lds_sync();
     // Scores that are -inf (NaN), or 0 because all summaries or all of the
     // position's queries are, need no second look: their indices decide.
     const bool finite = e2 < -kNegInf;
@@ -478,7 +481,7 @@ __device__ __forceinline__ void choose_many(const Choice& a) {
         const int n = base + lane;
         const bool tie = n < c1 && sc[min(n, c1 - 1)] == least;
         const unsigned long long m = __ballot(tie);
-        const int rank = (int)__popcll(m & ((1ull << lane) - 1));
+        const int rank = rank_in(m);
         if (tie) sc[n] = rank < want ? -kNegInf : kNegInf;
         want = max(want - (int)__popcll(m), 0);
       }
@@ -490,10 +493,10 @@ __device__ __forceinline__ void choose_many(const Choice& a) {
     T = ordered(thr);
   }
   int at = 0;
-  keys.each([&](int i, uint32_t x) {
+  scores.each_key([&](int i, uint32_t x) {
     const bool take = x >= T;
     const unsigned long long m = __ballot(take);
-    const int slot = at + (int)__popcll(m & ((1ull << lane) - 1));
+    const int slot = rank_in(m, at);
     if (take && slot < need) a.out[slot] = c0 + 64 * i + lane;
     at += (int)__popcll(m);
   });
@@ -510,7 +513,7 @@ void block_select_kernel(SelectParams a) {
   __shared__ __align__(16) float fixed_lds[LDS > 0 ? LDS : 4];
   float* const scores = LDS > 0 ? fixed_lds : launch_lds;  // [pos][stride]
   __shared__ __align__(16) u32x4_t tiles[NW][128];
-  __shared__ unsigned long long scratch[NW][66];
+  __shared__ int scratch[NW][66];
   __shared__ float norms[NW];
   __shared__ uint32_t nonzero[NW];
   const int lane = threadIdx.x & 63;
@@ -637,14 +640,15 @@ void block_select_kernel(SelectParams a) {
                 acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                     __builtin_bit_cast(bf16x8_t, qf[t][k]), __builtin_bit_cast(bf16x8_t, sf[k]),
                     acc[t], 0, 0, 0);
-            // Lane: block n + c, rows 4 kg + i of each tile. The maxima pass over a NaN.
+            // Lane: block n + c, rows 4 kg + i of each tile. The maxima pass over NaN and
+            // end at -inf.
 #pragma unroll
             for (int t = 0; t < CT; ++t)
 #pragma unroll
               for (int i = 0; i < PER; ++i) {
-                float x = acc[t][i * (4 / PER)];
+                float x = kNegInf;
 #pragma unroll
-                for (int e = 1; e < 4 / PER; ++e) x = fmaxf(x, acc[t][i * (4 / PER) + e]);
+                for (int e = 0; e < 4 / PER; ++e) x = fmaxf(x, acc[t][i * (4 / PER) + e]);
                 float u, v;
                 if constexpr (GP >= 8) {
                   lane_pair<16>(x, u, v);
@@ -709,7 +713,7 @@ void block_select_kernel(SelectParams a) {
     for (int i = lane; i < c0; i += 64) out[i] = i;
     for (int i = c1 + lane; i <= cur; i += 64) out[a.K - 1 - (cur - i)] = i;
     if (ch.need == 0) continue;
-    lds_u64* const words = (lds_u64*)scratch[wave];
+    lds_int* const words = (lds_int*)scratch[wave];
     const bool done = c1 - c0 <= 64 * 4    ? choose<D, 4>(ch, words)
                       : c1 - c0 <= 64 * 16 ? choose<D, 16>(ch, words)
                                            : choose<D, 0>(ch, words);
