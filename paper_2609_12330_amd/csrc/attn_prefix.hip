@@ -14,6 +14,7 @@
 // workgroup walks the prefix and then the own keys of its sequence in one loop and
 // writes the finished rows.
 #include "roll_tiles.hpp"
+#include "wave_ops.hpp"
 
 namespace ef {
 
@@ -52,22 +53,6 @@ struct TwoRuns {
       l.template load<ISK>(stage, t.base - off, t.end - off);
   }
 };
-
-// Smallest value of x over the wave, in DPP moves and lane swaps.
-__device__ __forceinline__ int wave_min_int(int x) {
-  auto mov = [](int v, auto ctrl) {
-    return __float_as_int(dpp_mov<decltype(ctrl)::value>(__int_as_float(v)));
-  };
-  x = min(x, mov(x, std::integral_constant<int, kDppQuadXor1>{}));
-  x = min(x, mov(x, std::integral_constant<int, kDppQuadXor2>{}));
-  x = min(x, mov(x, std::integral_constant<int, kDppHalfMirror>{}));
-  x = min(x, mov(x, std::integral_constant<int, kDppRowRor8>{}));
-  float a, b;
-  lane_pair<16>(__int_as_float(x), a, b);
-  x = min(__float_as_int(a), __float_as_int(b));
-  lane_pair<32>(__int_as_float(x), a, b);
-  return __builtin_amdgcn_readfirstlane(min(__float_as_int(a), __float_as_int(b)));
-}
 
 template <int D, int NW>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
@@ -139,7 +124,8 @@ void attn_prefix_kernel(PrefixParams a) {
     mask.lim = !valid     ? -1
                : a.causal ? sq + a.Lp + sequence_length(a.lengths, b, a.Skv) - a.Sq
                           : 0x7fffffff;  // the last key the row sees
-    tl.full_lo = wave_min_int(valid ? mask.lim : 0x7fffffff);
+    tl.full_lo =
+        __builtin_amdgcn_readfirstlane(wave_min(valid ? mask.lim : 0x7fffffff));
   };
   // The floor keeps a zero scale well defined (every visible key gets weight 1).
   roll_tiles<D, false>(tl, last - tl.first, mt * BM + wave * 32 < rows, Stages{sk0, sk1, sv0, sv1},

@@ -83,6 +83,7 @@ __device__ __forceinline__ void roll_tiles(const Tiles& tiles, int n, bool activ
   tiles.template load<true>(st.k0, t0);
   tiles.template load<false>(st.v0, t0);
   tiles.template load<true>(st.k1, t1);
+  tiles.template load<false>(st.v1, t1);  // all four stages are free: a short walk waits once
   ready();
   t0 = tile(0);
   t1 = tile(1);
@@ -102,7 +103,7 @@ __device__ __forceinline__ void roll_tiles(const Tiles& tiles, int n, bool activ
   for (int u = 0; u < steps; u += 2) {
     t2 = tile(u + 2);
     tiles.template load<true>(st.k0, t2);
-    tiles.template load<false>(st.v1, t1);
+    if (u > 0) tiles.template load<false>(st.v1, t1);
     if (active)
       pair_compute<D, false>(st.k1, st.v0, ro, t0, t1, 2 * u + 2 < nsub, top, mask, xa, xb, pa,
                              pb, tiles.on(u), tiles.on(min(u + 1, n - 1)));
