@@ -189,10 +189,10 @@ struct PrefixPlan {
 
 constexpr int kPrefixRows = 128;  // rows per workgroup
 
-// `tiles` tiles in about `parts` parts of at least `least` tiles: tiles per part.
-int tiles_per_part(long long tiles, long long parts, int least) {
+// `tiles` tiles in at most `parts` parts: tiles per part.
+int tiles_per_part(long long tiles, long long parts) {
   const long long p = std::max(parts, 1LL);
-  return (int)std::max<long long>((tiles + p - 1) / p, std::min<long long>(least, tiles));
+  return (int)((tiles + p - 1) / p);
 }
 
 PrefixPlan prefix_plan(const Shape& s, int Lp) {
@@ -208,20 +208,25 @@ PrefixPlan prefix_plan(const Shape& s, int Lp) {
     return p;
   }
   // Workgroups of the prefix: one to a compute unit keeps the matrix cores busy; half as
-  // many where the own keys have most of the work, which then get three of four places.
-  // 256 / 128 workgroups (us; 32/8 heads of 128, own keys half of the capacity in the
-  // mean; the prefix's part of the tiles in brackets): 64 sequences, 32768 + 2048 keys
-  // [0.33] 106 / 98, 16384 + 1024 [0.33] 57.7 / 54.9, 32 of them [0.33] 41 / 35, 16 [0.5]
-  // 27.2 / 28.0, 8 [0.67] 19.6 / 26.1, 64 over 32768 + 64 [0.94] 52 / 83.
+  // many where the own keys have most of the work, which then get three of four places;
+  // two where the prefix is nearly all and long. 256 / 128 workgroups (us; 32/8 heads of
+  // 128, own keys half of the capacity in the mean; the prefix's part of the tiles in
+  // brackets): 64 sequences, 32768 + 2048 keys [0.33] 106 / 98, 16384 + 1024 [0.33] 57.7 /
+  // 54.9, 32 of them [0.33] 41 / 35, 16 [0.5] 27.2 / 28.0, 8 [0.67] 19.6 / 26.1, 64 over
+  // 32768 + 64 [0.94] 52 / 83. 256 / 512: 16 sequences, 64000 + 64 keys [31 tiles to each
+  // of 256] 70 / 59, 32 of them 73 / 63, 16 over 16000 + 100 [8] 20.0 / 24.0.
   const long long w1 = np * s.Hkv * p.mt1, w2 = no * heads * p.mt2;
-  const long long n1 = kFillWgs / (5 * w1 >= 3 * (w1 + w2) ? 2 : 4);
+  const bool mostly = 5 * w1 >= 3 * (w1 + w2);
+  const long long n1 = !mostly ? kFillWgs / 4
+                       : p.mt1 == 1 && w1 >= 24 * (kFillWgs / 2) ? kFillWgs
+                                                                 : kFillWgs / 2;
   if (np > 0) {
-    p.T1 = tiles_per_part(np, n1 / (s.Hkv * (long long)p.mt1), 2);
+    p.T1 = tiles_per_part(np, n1 / (s.Hkv * (long long)p.mt1));
     p.P1 = (int)((np + p.T1 - 1) / p.T1);
     p.n_prefix = (long long)s.Hkv * p.mt1 * p.P1;
   }
   if (no > 0) {
-    p.T2 = tiles_per_part(no, kFillWgs / (heads * p.mt2), 4);
+    p.T2 = tiles_per_part(no, (kFillWgs - p.n_prefix) / (heads * p.mt2));
     p.P2 = (int)((no + p.T2 - 1) / p.T2);
     p.n_own = heads * p.mt2 * p.P2;
   }
