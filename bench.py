@@ -443,7 +443,7 @@ def measure(cfg, args, ef, wl, torch, dev, seed, cpu_budget, clock=None):
             "_local" if cfg.local else "") + (f"_dsplit{DS}" if DS > 0 else "") + (
             "_fused" if fused and P > 1 else "")
         src = source_hash(*(("decode_split.hip", "group_combine.hpp") if valu
-                            else ("attn_mfma.hip",)), "ef_device.hpp")
+                            else ("attn_mfma.hip", "rolling.hpp")), "ef_device.hpp")
         alg = cfg.algorithmic_bytes() if single_call else kv + q_bytes
         achieved = alg / (prod_avg * 1e-3) / 1e9
         roof = {"bound": "hbm", "achieved": round(achieved, 1), "peak": HBM_PEAK_GBS,
@@ -458,7 +458,7 @@ def measure(cfg, args, ef, wl, torch, dev, seed, cpu_budget, clock=None):
     else:
         kernel = "attn_mfma" + ("_local" if cfg.local else "") + (
             ("_split_diff" if P > 1 else "_diff") if cfg.diff else "")
-        src = source_hash("attn_mfma.hip", "ef_device.hpp")
+        src = source_hash("attn_mfma.hip", "rolling.hpp", "ef_device.hpp")
         # A split differential layer launches the producer once per branch.
         flops = cfg.flops() // (2 if cfg.diff and P > 1 else 1)
         achieved = flops / (prod_avg * 1e-3) / 1e12
