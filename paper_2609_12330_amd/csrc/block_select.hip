@@ -26,8 +26,14 @@
 // border too. Where that does not apply (need > 64, or more than 64 such scores) the
 // second bisection counts all scores; a border of more than 64 (many equal scores) is
 // settled in LDS.
-#include "ef_long.hpp"
+//
+// What bounds it: 4096 queries of 32/8 heads of 128, 16 of up to 1024 blocks (33 GFLOP),
+// 102 us: vector instructions (3600 in a wave of 16 rows, besides 1900 scalar ones), a
+// little more than half for the scores, the rest for the choice; the matrix cores are
+// 12% busy. One token of 16 sequences, 32 of 1024 blocks (25 MB), 11.6 us: launch, the
+// summaries' loads, and one wave's choice, one after the other.
 #include "ef_device.hpp"
+#include "ef_long.hpp"
 #include "wave_ops.hpp"
 
 #include <type_traits>
@@ -516,8 +522,9 @@ void block_select_kernel(SelectParams a) {
       }
   };
   // The lane's part of a tile as the product takes it: block c, elements 32 k + 8 kg on.
-  // A load covers eight blocks' 128-byte lines (16 blocks to a quarter of a wave cost
-  // the address unit a lookup a lane, 16 a load instead of 2: ?).
+  // A load covers eight blocks' 128-byte lines; fragments read straight from memory touch
+  // 16 lines in each quarter of a wave (with the score rows written without conditions,
+  // one-token choice 15.7 -> 11.6 us, 4096 queries 130 -> 106).
   // The 64-element halves of a tile turn in a 2 KiB buffer of the wave, 16-byte chunks
   // permuted by row against bank conflicts; LDS keeps a wave's operations in order.
   auto turn = [&](const u32x4_t (&x)[KS], u32x4_t (&y)[KS]) {

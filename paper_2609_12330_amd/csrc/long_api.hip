@@ -155,6 +155,12 @@ constexpr long long kFillWgs = 512;
 // of 512, 32/8 heads of 128; lists of neighbours alike, then independent): 4096 queries
 // 180 / 131, 2048 [512 workgroups of 128] 89 / 69 and 479 / 580, 1024 [256] 46.6 / 45.0
 // and 251 / 378, 512 38.8 / 38.6 and 138 / 200.
+//
+// `fused`: the last of P workgroups to store a state combines its head's rows, where
+// these states are few; otherwise a second kernel does, at 2 to 2.5 us between two
+// launches. Kernels' time alone, one / two (us; rows x P in brackets): one sequence over
+// 8, 16, 32, 64 blocks [32 to 256] 9.3 / 10.0, 10.6 / 10.7, 12.0 / 11.2, 15.9 / 14.8, 16
+// over 32 [16] 28.5 / 30.9, four tokens over 16, 64 [256, 1024] 18.3 / 15.3, 34 / 19.
 struct BlocksPlan {
   int bm, mtiles, P;
   bool fused;
@@ -201,7 +207,16 @@ PrefixPlan prefix_plan(const Shape& s, int Lp) {
   const long long np = (Lp + 63) / 64, no = ((long long)s.Skv + 63) / 64;
   p.mt1 = (int)((s.B * R + kPrefixRows - 1) / kPrefixRows);
   p.mt2 = (int)((R + kPrefixRows - 1) / kPrefixRows);
-  p.whole = np + no == 0 || (R >= 64 && heads * p.mt2 >= 192);
+  // `whole` spares the states and their combine, which take a row about as long as 32
+  // tiles do, but walks the prefix for the empty rows of its tiles too, and needs rows
+  // for the chip. Split / whole (us; 32/8 heads of 128; sequences x tokens, prefix + 256 or
+  // 1024 keys): 24 x 32 over 2048 62 / 49, over 16384 343 / 330; 16 x 32 over 2048 42 / 46,
+  // over 16384 191 / 301; 64 x 64 over 2048 258 / 163; with half of the rows empty 64 x 16
+  // over 2048 73 / 65, over 16384 392 / 485, 32 x 16 over 2048 42 / 45; 16 x 100 over 700
+  // 70 / 39, over 9000 290 / 316.
+  p.whole = np + no == 0 ||
+            (heads * R >= 192LL * kPrefixRows &&
+             (p.mt2 * (long long)kPrefixRows - R) * np <= 32 * R);
   if (p.whole) {
     p.P2 = p.P = 1;
     p.n_own = heads * p.mt2;

@@ -26,7 +26,7 @@ SHAPES = [
     (37, 8, 8, 3, 2000, 100, 64, True, None),        # packed rows of more than one tile
     (2, 64, 8, 16, 4000, 900, 128, True, [900, 100]),
     (3, 16, 2, 100, 700, 100, 128, True, None),
-    (25, 32, 8, 30, 650, 30, 64, True, None),        # whole walks: rows fill the chip
+    (26, 32, 8, 30, 650, 30, 64, True, None),        # whole walks: rows fill the chip
     (24, 16, 8, 70, 333, 90, 128, True, [90 - i for i in range(24)]),
     (24, 16, 8, 64, 130, 64, 128, False, [64 - i for i in range(24)]),
     (2, 40, 10, 500, 77, 500, 64, True, [500, 20]),
