@@ -19,19 +19,20 @@
 // is to 2^-53), in index order, and the best of them complete the list.
 //
 // The need-th largest of the scores, every 64th in a lane's registers, is bounded from
-// below by the need-th largest of the lanes' largest ones, which a bisection between
-// their smallest and largest finds, each step one ballot (a somewhat lower bound does,
-// so it stops early). The few scores above that bound less 2 E then go one to a lane,
-// in index order, for a second bisection. They hold every block within 2 E of the
-// border too. Where that does not apply (need > 64, or more than 64 such scores) the
-// second bisection counts all scores; a border of more than 64 (many equal scores) is
-// settled in LDS.
+// below by the need-th largest of the lanes' largest ones. The few scores above that bound
+// less 2 E, which hold every block within 2 E of the border too, then go one to a lane, in
+// index order. In both lists each lane finds its rank by comparing its score with all of
+// them (a bisection by ballots is a chain of dependent steps: 4096 queries of 256 blocks
+// 70 -> 61 us). Where that does not apply (need > 64, or more than 64 such scores) a
+// bisection counts all scores; a border of more than 64 (many equal scores) is settled in
+// LDS.
 //
 // What bounds it: 4096 queries of 32/8 heads of 128, 16 of up to 1024 blocks (33 GFLOP),
-// 102 us: vector instructions (3600 in a wave of 16 rows, besides 1900 scalar ones), a
-// little more than half for the scores, the rest for the choice; the matrix cores are
-// 12% busy. One token of 16 sequences, 32 of 1024 blocks (25 MB), 11.6 us: launch, the
-// summaries' loads, and one wave's choice, one after the other.
+// 100 us, 62 of them the scores and 38 the choice (10 of these the exact scores, which
+// about 1% of the positions need): instructions, with two waves on a SIMD; the matrix
+// cores are 12% busy. Two positions chosen step by step together need so many registers
+// that it takes longer. One token of 16 sequences, 32 of 1024 blocks (25 MB), 11.5 us:
+// launch, the summaries' loads, and one wave's choice, one after the other.
 #include "ef_device.hpp"
 #include "ef_long.hpp"
 #include "wave_ops.hpp"
@@ -48,6 +49,7 @@ namespace {
 typedef __attribute__((address_space(3))) float lds_float;
 typedef __attribute__((address_space(3))) int lds_int;
 typedef __attribute__((address_space(3))) u32x4_t lds_chunk;
+typedef __attribute__((address_space(3))) floatx4 lds_float4;
 
 // Order-preserving integer of a float (no NaN).
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -90,7 +92,8 @@ __device__ __forceinline__ double pair_max64(double x) {
 // score(n) in 64 bits, by one wave, the same in every lane; NaN counts as -inf. 16
 // lanes take a head, four heads at a time.
 template <int D>
-__device__ __forceinline__ double exact_score(const uint16_t* q, size_t head_stride, int G, const uint16_t* s) {
+__device__ __forceinline__ double exact_score(const uint16_t* q, size_t head_stride, int G,
+                                              const uint16_t* s) {
   constexpr int W = D / 32;  // words of two elements per lane
   const int lane = threadIdx.x & 63;
   const int sub = lane & 15;
@@ -132,8 +135,9 @@ __device__ __forceinline__ bool all_zero(const uint16_t* q, size_t head_stride, 
 // [lo, hi], by exact score: their scores become +inf, the others' -inf. The best
 // so far are held by the lanes, entry i in slot i / 64 of lane i % 64.
 template <int D>
-__device__ __forceinline__ void settle_border(lds_float* sc, int c0, int c1, float lo, float hi, int want,
-                              const uint16_t* q, size_t head_stride, int G, const uint16_t* s) {
+__device__ __forceinline__ void settle_border(lds_float* sc, int c0, int c1, float lo, float hi,
+                                              int want, const uint16_t* q, size_t head_stride,
+                                              int G, const uint16_t* s) {
   constexpr int SLOTS = kMaxTopk / 64;
   const int lane = threadIdx.x & 63;
   double val[SLOTS];
@@ -263,8 +267,7 @@ __device__ __forceinline__ uint32_t bisect(uint32_t lo, uint32_t hi, int need, i
 }
 
 // One position's choice among the blocks [c0, c1), which are more than the `need` wanted
-// ones, by one wave. sc: the scores; bound: their
-// largest error.
+// ones, by one wave. sc: the scores; bound: their largest error.
 struct Choice {
   lds_float* sc;
   int c0, c1, need;
@@ -304,10 +307,41 @@ struct Choice {
   }
 };
 
+// How many of n scores in LDS (whole groups of 16, filled with -inf) are above x: their
+// ranks by comparing each with each, two instructions a score, without a chain of
+// dependent steps.
+__device__ __forceinline__ int above(const lds_float* keys, int n, float x) {
+  int rank = 0;
+  for (int j = 0; j < n; j += 16) {
+    floatx4 k[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) k[e] = reinterpret_cast<const lds_float4*>(keys + j)[e];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) rank += k[e / 4][e % 4] > x ? 1 : 0;
+  }
+  return rank;
+}
+
+// x of the lowest lane of the set.
+__device__ __forceinline__ float lane_of(float x, unsigned long long set) {
+  return __builtin_bit_cast(
+      float, __builtin_amdgcn_readlane(__float_as_int(x), __builtin_ctzll(set)));
+}
+
+// The need-th largest of the lanes' x, from their ranks; equal ones have the same rank.
+__device__ __forceinline__ float nth(float x, int rank, int need) {
+  unsigned long long m = 0;
+  for (int r = need - 1; m == 0; --r) m = __ballot(rank == r);  // rank 0 is always there
+  return lane_of(x, m);
+}
+
 // The choice by fp32 scores, and by exact ones where few scores come into question; false,
-// with nothing written, where exact scores of more than 64 blocks are called for. scratch: 65 words of LDS.
+// with nothing written, where exact scores of more than 64 blocks are called for.
+// scratch: 128 words of LDS of the wave.
 template <int D, int NV>
 __device__ __forceinline__ bool choose(const Choice& a, lds_int* scratch) {
+  lds_float* const keys = (lds_float*)scratch;
+  lds_int* const blocks = scratch + 64;
   const int lane = threadIdx.x & 63;
   const int c0 = a.c0, c1 = a.c1, need = a.need;
   Scores<NV> scores{a.sc, c0, c1, {}};
@@ -318,61 +352,63 @@ __device__ __forceinline__ bool choose(const Choice& a, lds_int* scratch) {
       float, __builtin_amdgcn_readfirstlane(__float_as_int(wave_max(best))));
   const uint32_t top = ordered(most_of_all);
   // The few scores that can be in or near the border, one to a lane, in index order.
-  uint32_t few = 0;
+  float few = kNegInf;
   int few_block = c0 + lane, held = c1 - c0;
   if (held <= 64) {
-    few = scores.has(0) ? ordered(scores.fetch(0)) : 0u;
+    if (lane < held) few = scores.fetch(0);
+    keys[lane] = few;
   } else if (need <= 64) {
-    float least = -wave_max(-best);
-    float hi = most_of_all;
-    for (int k = 64, most = need + (64 - need) / 8, step = 0; k > most && step < 16; ++step) {
-      const float mid = 0.5f * least + 0.5f * hi;
-      const int n = (int)__popcll(__ballot(best >= mid));
-      if (n >= need && mid > least) {
-        least = mid;
-        k = n;
-      } else {
-        hi = mid;  // (NaN with infinite ends: no further step changes anything)
-      }
-    }
+    keys[lane] = best;
+    wave_lds_sync();
+    const float least = nth(best, above(keys, 64, best), need);
+    wave_lds_sync();  // read before they are written again
     // (Minus an infinite bound this is -inf, or NaN: then they are not few.)
     const float base = least - fmaxf(a.apart(least), a.apart(most_of_all));
     held = 0;
-    scores.each([&](int i, float x) {
-      const unsigned long long m = __ballot(x >= base);
-      // Word 64 takes what has no place.
-      scratch[x >= base ? min(rank_in(m, held), 64) : 64] = c0 + 64 * i + lane;
-      held += (int)__popcll(m);
-    });
+    scores.each([&](int, float x) { held += (int)__popcll(__ballot(x >= base)); });
     if (!(base > kNegInf)) held = 65;
-    wave_lds_sync();
-    if (lane < held) few_block = scratch[lane];
-    if (lane < held && held <= 64) few = ordered(a.sc[few_block]);
-    wave_lds_sync();  // read before the wave's next position writes
+    if (held <= 64) {
+      keys[lane] = kNegInf;
+      int at = 0;
+      scores.each([&](int i, float x) {
+        const unsigned long long m = __ballot(x >= base);
+        if (x >= base) {
+          const int slot = rank_in(m, at);
+          keys[slot] = x;
+          blocks[slot] = c0 + 64 * i + lane;
+        }
+        at += (int)__popcll(m);
+      });
+      wave_lds_sync();
+      few = keys[lane];
+      few_block = lane < held ? blocks[lane] : 0;
+    }
   }
   if (held <= 64) {
-    int cnt = held;
-    const uint32_t T =
-        bisect(__builtin_amdgcn_readfirstlane(wave_min(lane < held ? few : 0xffffffffu)), top,
-               need, cnt, [&](uint32_t t) { return (int)__popcll(__ballot(few >= t)); });
-    bool take = few >= T;
+    wave_lds_sync();
+    const int rank = above(keys, held, few);
+    bool take = rank < need;
+    const unsigned long long taken = __ballot(take);
     // Last score in, first one out (where that is none of the few, more than e2 below).
-    const float least = unordered(wave_min(take ? few : 0xffffffffu));
-    const uint32_t second = wave_max(take ? 0u : few);
+    const float least = nth(few, rank, need);
+    const unsigned long long out = __ballot(rank == need);
     const float e2 = a.apart(least);
-    if (__builtin_expect(
-            cnt != need || (second != 0 && !(least - unordered(second) > e2)), 0)) {
-      const float x = unordered(few);
+    // More than `need` have rank < need where equal ones are at the border.
+    if (__builtin_expect((int)__popcll(taken) != need ||
+                             (held > need && !(least - lane_of(few, out) > e2)),
+                         0)) {
+      const bool here = lane < held;
       const bool finite = e2 < -kNegInf && least > kNegInf;
-      const bool sure = few != 0 && finite && x > least + e2;
-      const bool near = few != 0 && !sure && (!finite || x >= least - e2);
+      const bool sure = here && finite && few > least + e2;
+      const bool near = here && !sure && (!finite || few >= least - e2);
       const unsigned long long todo = __ballot(near);
       const int want = need - (int)__popcll(__ballot(sure));
-      const int rank = a.template exact_rank<D>(todo, few_block);
-      take = sure || (near && rank < want);
+      const int exact = a.template exact_rank<D>(todo, few_block);
+      take = sure || (near && exact < want);
     }
     const int slot = rank_in(__ballot(take));
     if (take && slot < need) a.out[slot] = few_block;
+    wave_lds_sync();  // read before the wave's next position writes
     return true;
   }
 
@@ -496,7 +532,7 @@ void block_select_kernel(SelectParams a) {
   __shared__ __align__(16) float fixed_lds[LDS > 0 ? LDS : 4];
   float* const scores = LDS > 0 ? fixed_lds : launch_lds;  // [pos][stride]
   __shared__ __align__(16) u32x4_t tiles[NW][128];
-  __shared__ int scratch[NW][66];
+  __shared__ __align__(16) int scratch[NW][128];
   __shared__ float norms[NW];
   __shared__ uint32_t nonzero[NW];
   const int lane = threadIdx.x & 63;

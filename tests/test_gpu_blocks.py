@@ -90,7 +90,10 @@ SELECTS = [
     (1, 20, 1, 9, 2100, 128, 64, 9, 1, 1, None),    # groups of 20, two column tiles
     (1, 32, 1, 3, 5000, 64, 64, 32, 1, 2, None),    # groups of 32
     (1, 3, 3, 130, 2000, 128, 64, 5, 4, 1, None),   # every choice forced
-    (2, 4, 2, 2000, 2000, 64, 64, 7, 1, 1, None),   # four column tiles
+    (2, 4, 2, 2000, 2000, 64, 64, 7, 1, 1, None),
+    (2, 16, 2, 2000, 9000, 64, 64, 7, 1, 1, None),  # four column tiles
+    (3, 8, 2, 1403, 9000, 128, 64, 9, 0, 1, [9000, 1403, 5000]),
+    (1, 4, 2, 9, 100000, 128, 64, 16, 1, 2, None),  # scores that stay in LDS
     (1, 16, 16, 300, 2000, 128, 128, 6, 1, 1, None),
     (1, 4, 2, 40, 33000, 128, 64, 256, 1, 1, None),  # the longest list
     (1, 2, 1, 2, 1023999, 64, 64, 40, 1, 2, None),  # as many blocks as there may be
