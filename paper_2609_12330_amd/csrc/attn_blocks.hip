@@ -31,19 +31,20 @@ namespace {
 constexpr int kWords = (kMaxBlocks + 31) / 32;
 constexpr int kWindow = 512;  // blocks of the union that are walked at a time
 
-// Union of the lists of the workgroup's positions.
+// Union of the lists of the workgroup's positions, at most one to a row.
+template <int NW>
 struct UnionList {
-  uint32_t word[kWords];  // bitmap
-  int before[kWords];     // blocks below each word
-  int block[kWindow];     // the window's blocks, ascending
-  uint32_t mask[kWindow][2];  // positions that selected them
-  int waves[4];
+  uint32_t word[kWords];       // bitmap
+  int before[kWords];          // blocks below each word
+  int block[kWindow];          // the window's blocks, ascending
+  uint32_t mask[kWindow][NW];  // positions that selected them
+  int waves[NW];
 };
 
 template <int D, int NW>
 struct ListTiles {
   StageLoader<D, NW, NW> ld;
-  const UnionList* u;
+  const UnionList<NW>* u;
   int shift;    // log2 of the keys per block
   int cend;     // keys any row sees
   int full_lo;  // keys up to it are visible to all rows, as far as selected
@@ -102,7 +103,7 @@ void attn_blocks_kernel(BlocksParams a) {
   fr.init(lane);
   constexpr int STAGE = 2 * Geo::SUB;
   __shared__ __align__(1024) char sk0[STAGE], sk1[STAGE], sv0[STAGE], sv1[STAGE];
-  __shared__ UnionList u;
+  __shared__ UnionList<NW> u;
   ListTiles<D, NW> tl;
   const size_t head = (size_t)bh * a.Skv * D;
   tl.ld.init(a.k + head, a.v + head, wave, wave);
@@ -165,7 +166,8 @@ void attn_blocks_kernel(BlocksParams a) {
       for (int rank = u.before[i] - f; bits; ++rank, bits &= bits - 1)
         if (rank >= 0 && rank < n) {
           u.block[rank] = 32 * i + __builtin_ctz(bits);
-          u.mask[rank][0] = u.mask[rank][1] = 0;
+#pragma unroll
+          for (int w = 0; w < NW; ++w) u.mask[rank][w] = 0;
         }
     }
     __syncthreads();

@@ -198,6 +198,9 @@ ATTENTION = [
     (1, 2, 2, 64, 64 * 700, 64, 64, 16, None, False),  # a union of more than one window
     (1, 2, 2, 3, 64 * 1500, 64, 64, 250, None, False),  # ... and split over workgroups
     (1, 4, 4, 150, 128 * 300, 128, 128, 12, None, True),
+    (1, 32, 32, 2048, 2100, 64, 64, 4, None, True),    # 128 positions to a tile
+    (2, 16, 16, 2049, 2100, 128, 128, 3, [2100, 2060], False),
+    (1, 64, 32, 1030, 4000, 64, 64, 9, None, False),   # 64 positions to a tile of 128 rows
 ]
 
 
