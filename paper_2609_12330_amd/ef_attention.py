@@ -674,6 +674,16 @@ def _call_on(t, stream, fn, *args):
         return fn(*args, _stream_handle(stream))
 
 
+def _new(shape, dtype, t, stream):
+    """An uninitialised tensor on t's device, in the memory of the stream the call runs on: freed,
+    it serves later work of that stream only."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=t.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=t.device)
+
+
 def num_blocks(Skv: int, block_size: int = 64) -> int:
     """Blocks of a key axis of Skv keys."""
     return -(-Skv // block_size)
@@ -694,7 +704,7 @@ def block_summary(k, block_size: int = 64, lengths=None, new_keys: int = 0, out=
     if out is None:
         if new_keys:
             raise ValueError("new_keys needs out, the summaries of the other blocks")
-        out = torch.empty(shape, dtype=torch.bfloat16, device=k.device)
+        out = _new(shape, torch.bfloat16, k, stream)
     else:
         _check_tensor(out, "out", torch.bfloat16, 4, k)
         if out.shape != shape:
@@ -722,7 +732,7 @@ def block_select(q, summary, Skv: int, topk: int, block_size: int = 64, sink_blo
                          f"got {tuple(summary.shape)}")
     shape = (B, Hkv, Sq, topk)
     if out is None:
-        out = torch.empty(shape, dtype=torch.int32, device=q.device)
+        out = _new(shape, torch.int32, q, stream)
     else:
         _check_tensor(out, "out", torch.int32, 4, q)
         if out.shape != shape:
@@ -740,33 +750,39 @@ def _same_devices(q, k, v):
         _same_device(v, q, "v")
 
 
-def _out_bf16(q, out):
+def _out_bf16(q, out, stream):
     torch = _torch()
     if out is None:
-        return torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        return _new(q.shape, torch.bfloat16, q, stream)
     _check_tensor(out, "out", torch.bfloat16, 4, q)
     if out.shape != q.shape:
         raise ValueError("out must be shaped like q")
     return out
 
 
-def _state_workspace(n, q):
+def _state_workspace(n, q, stream=None):
     """n bytes on q's device, the arrival counters at their start zero (they stay zero from call
-    to call); None for 0 bytes."""
+    to call); None for 0 bytes. With a stream both the memory and its clearing are that
+    stream's."""
     if n == 0:
         return None
-    workspace = _torch().empty(n, dtype=_torch().uint8, device=q.device)
-    workspace[:COUNTER_REGION_BYTES].zero_()
+    torch = _torch()
+    workspace = _new((n,), torch.uint8, q, stream)
+    if stream is None:
+        workspace[:COUNTER_REGION_BYTES].zero_()
+    else:
+        with torch.cuda.stream(stream):
+            workspace[:COUNTER_REGION_BYTES].zero_()
     return workspace
 
 
-def _own_workspace(workspace, size, sizes, q):
+def _own_workspace(workspace, size, sizes, q, stream):
     """(pointer, bytes, tensor) of the workspace given, or of a new one of size(*sizes) bytes."""
     if workspace is None:
         n = size(*sizes)
         if n == 0:
             return None, 0, None
-        workspace = _state_workspace(n, q)
+        workspace = _state_workspace(n, q, stream)
     if workspace.get_device() != q.get_device() or not workspace.is_contiguous():
         _check_workspace(workspace, q)
     return workspace.data_ptr(), workspace.nbytes, workspace
@@ -794,10 +810,10 @@ def attention_blocks(q, k, v, blocks, block_size: int = 64, scale: Optional[floa
         raise ValueError(f"blocks must be [{B}, {Hkv}, {Sq}, topk], got {tuple(blocks.shape)}")
     if scale is None:
         scale = 1.0 / math.sqrt(D)
-    o = _out_bf16(q, out)
+    o = _out_bf16(q, out, stream)
     ptr, n, workspace = _own_workspace(
         workspace, ef_attention_blocks_workspace_size, (B, Hq, Hkv, Sq, Skv, D, block_size, topk),
-        q)
+        q, stream)
     st = _call_on(q, stream, ef_attention_blocks, q.data_ptr(), k.data_ptr(), v.data_ptr(),
                   blocks.data_ptr(), _lengths_ptr(lengths, B, q), o.data_ptr(), B, Hq, Hkv, Sq,
                   Skv, D, float(scale), block_size, topk, ptr, n)
@@ -829,9 +845,10 @@ def attention_shared_prefix(q, k_prefix, v_prefix, k, v, scale: Optional[float] 
         raise ValueError("k_prefix and v_prefix must be [Hkv, Lp, D] matching k")
     if scale is None:
         scale = 1.0 / math.sqrt(D)
-    o = _out_bf16(q, out)
+    o = _out_bf16(q, out, stream)
     ptr, n, workspace = _own_workspace(
-        workspace, ef_attention_shared_prefix_workspace_size, (B, Hq, Hkv, Sq, Lp, Skv, D), q)
+        workspace, ef_attention_shared_prefix_workspace_size, (B, Hq, Hkv, Sq, Lp, Skv, D), q,
+        stream)
     st = _call_on(q, stream, ef_attention_shared_prefix, q.data_ptr(), k_prefix.data_ptr(),
                   v_prefix.data_ptr(), k.data_ptr(), v.data_ptr(), _lengths_ptr(lengths, B, q),
                   o.data_ptr(), B, Hq, Hkv, Sq, Lp, Skv, D, float(scale), causal, ptr, n)

@@ -159,6 +159,33 @@ def test_other_stream_and_shared_workspace():
         assert not ef.workspace_counters(ws).any()
 
 
+def test_other_stream_without_a_workspace():
+    """A call on another stream makes what it needs there: nothing of it waits for, or is
+    overtaken by, the work of the current stream."""
+    announce("other stream, own workspace")
+    B, Hq, H, D, S = 1, 8, 2, 128, 3000
+    q, k = normal(160, B, Hq, 1, D).cuda(), normal(161, B, H, S, D).cuda()
+    lists = ef.block_select(q, ef.block_summary(k), S, 12)
+    want = (ef.attention_blocks(q, k, k, lists), ef.attention_shared_prefix(q, k[0], k[0], k, k))
+    stream = torch.cuda.Stream()
+    busy = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    for i in range(3):
+        n = ef.make_blocks_workspace(q, k, 12).numel()
+        torch.full((n,), 255, dtype=torch.uint8, device="cuda")  # what its memory holds
+        for _ in range(20):
+            busy = (busy @ busy).clamp(-1, 1)
+        got = (ef.attention_blocks(q, k, k, lists, stream=stream),
+               ef.attention_shared_prefix(q, k[0], k[0], k, k, stream=stream))
+        for _ in range(20):  # would take the memory of a workspace freed here
+            busy = (busy @ busy).clamp(-1, 1)
+            torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+        stream.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), i
+        torch.cuda.synchronize()
+
+
 def test_counters_that_were_not_zero():
     announce("counters not zero")
     B, Hq, H, D, S = 1, 4, 1, 64, 2000
