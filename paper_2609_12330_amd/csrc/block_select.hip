@@ -649,7 +649,8 @@ void block_select_kernel(SelectParams a) {
             if (AHEAD > 1 && n >= scored) break;
             u32x4_t sf[KS];
             turn(now[j], sf);
-            mnorm = fmaxf(mnorm, norm2(sf));
+            const float n2 = norm2(sf);  // blocks that no position scores may hold anything
+            mnorm = fmaxf(mnorm, n + c < scored ? n2 : 0.f);
             floatx4 acc[CT];
 #pragma unroll
             for (int t = 0; t < CT; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};

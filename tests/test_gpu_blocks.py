@@ -94,6 +94,7 @@ SELECTS = [
     (2, 16, 2, 2000, 9000, 64, 64, 7, 1, 1, None),  # four column tiles
     (3, 8, 2, 1403, 9000, 128, 64, 9, 0, 1, [9000, 1403, 5000]),
     (1, 4, 2, 9, 100000, 128, 64, 16, 1, 2, None),  # scores that stay in LDS
+    (1, 4, 2, 5, 80000, 64, 64, 200, 2, 1, None),   # ... with a long list
     (1, 16, 16, 300, 2000, 128, 128, 6, 1, 1, None),
     (1, 4, 2, 40, 33000, 128, 64, 256, 1, 1, None),  # the longest list
     (1, 2, 1, 2, 1023999, 64, 64, 40, 1, 2, None),  # as many blocks as there may be
@@ -130,6 +131,21 @@ def test_select_where_fp32_cannot_tell():
     m[:, :, 100:] = m[:, :, :100].flip(2)
     ref = oracle.block_select_ref(f64(q), f64(m), S, K, bs, 1, 2)
     got = ef.block_select(q.cuda(), m.cuda(), S, K, bs, 1, 2)
+    torch.cuda.synchronize()
+    same_lists(got, ref)
+
+
+@pytest.mark.parametrize("junk", [float("inf"), float("nan"), 1e30])
+def test_select_does_not_read_the_last_summaries(junk):
+    """What stands in the summaries of the local blocks and behind the sequence does not matter."""
+    announce(f"select junk {junk}")
+    B, Hq, H, Sq, S, D, bs, K, local = 2, 8, 2, 1, 64 * 100, 128, 64, 12, 2
+    n = [64 * 70 + 5, 64 * 100]
+    q, m = normal(14, B, Hq, Sq, D), normal(15, B, H, 100, D)
+    ref = oracle.block_select_ref(f64(q), f64(m), S, K, bs, 1, local, n)
+    for b, x in enumerate(n):
+        m[b, :, (x - 1) // bs + 1 - local:] = junk
+    got = ef.block_select(q.cuda(), m.cuda(), S, K, bs, 1, local, lengths=lengths_of(n))
     torch.cuda.synchronize()
     same_lists(got, ref)
 
