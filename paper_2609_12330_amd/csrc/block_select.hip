@@ -233,9 +233,12 @@ struct Scores {
   __device__ __forceinline__ void each_key(F f) const {
     each([&](int i, float x) { f(i, has(i) ? ordered(x) : 0u); });
   }
+  // Scores from the value of `least` on (compared as floats, which cost no conversion; of
+  // -inf, where places without a block count too, and below it no use is made).
   __device__ __forceinline__ int count(uint32_t least) const {
+    const float t = unordered(least);
     int k = 0;
-    each_key([&](int, uint32_t x) { k += (int)__popcll(__ballot(x >= least)); });
+    each([&](int, float x) { k += (int)__popcll(__ballot(x >= t)); });
     return k;
   }
 };
@@ -354,6 +357,7 @@ __device__ __forceinline__ bool choose(const Choice& a, lds_int* scratch) {
   // The few scores that can be in or near the border, one to a lane, in index order.
   float few = kNegInf;
   int few_block = c0 + lane, held = c1 - c0;
+  uint32_t low = 0;  // no more than the need-th largest
   if (held <= 64) {
     if (lane < held) few = scores.fetch(0);
     keys[lane] = few;
@@ -362,6 +366,7 @@ __device__ __forceinline__ bool choose(const Choice& a, lds_int* scratch) {
     wave_lds_sync();
     const float least = nth(best, above(keys, 64, best), need);
     wave_lds_sync();  // read before they are written again
+    if (least > kNegInf) low = ordered(least);
     // (Minus an infinite bound this is -inf, or NaN: then they are not few.)
     const float base = least - fmaxf(a.apart(least), a.apart(most_of_all));
     held = 0;
@@ -413,8 +418,8 @@ __device__ __forceinline__ bool choose(const Choice& a, lds_int* scratch) {
   }
 
   // Too many for the lanes: the same on all scores, unless exact ones are called for.
-  int cnt = c1 - c0;
-  const uint32_t T = bisect(0, top, need, cnt, [&](uint32_t t) { return scores.count(t); });
+  int cnt = low ? scores.count(low) : c1 - c0;
+  const uint32_t T = bisect(low, top, need, cnt, [&](uint32_t t) { return scores.count(t); });
   uint32_t in = 0xffffffffu, outside = 0;
   scores.each_key([&](int, uint32_t x) {
     in = min(in, x >= T ? x : 0xffffffffu);
