@@ -259,7 +259,7 @@ __device__ __forceinline__ void combine_shared(const float* m, const float* l, c
           s[e] = w > 0.f ? fmaf(w, __uint_as_float(y[j][e]), s[e]) : s[e];
       }
     }
-    const float inv = L > 0.f ? 1.f / L : 0.f;
+    const float inv = L == 0.f ? 0.f : 1.f / L;  // NaN stays NaN
     const u32x2_t w = {pack_bf16x2(s[0] * inv, s[1] * inv), pack_bf16x2(s[2] * inv, s[3] * inv)};
     if (valid) *reinterpret_cast<u32x2_t*>(o + (row0 + r) * D + 4 * ch) = w;
   }

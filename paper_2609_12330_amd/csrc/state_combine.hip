@@ -5,8 +5,9 @@
 // One wave per row. Lane p holds the reference and sum of state p (64 at a time, a
 // running maximum carries over); each group of D / 4 lanes reads the value states of
 // every other (D = 128) or fourth (D = 64) partition, 16 bytes a lane, the first ones
-// requested before the weights are formed. A state without a key has weight 0 and what
-// stands in its place does not matter.
+// requested before the weights are formed. A state without a key has weight and sum 0 and
+// what stands in its value's place does not matter; a sum that is NaN (a query that is)
+// makes the row NaN.
 //
 // Bound by latency: 2048 rows of 10 states of 128 (11 MB) 4.8 us.
 #include "ef_device.hpp"
@@ -48,7 +49,7 @@ __global__ __launch_bounds__(kCombineWaves * 64) void state_combine_kernel(State
     const float ref = top == kNegInf ? 0.f : top;
     const float w = exp2_fast((m - ref) * kLog2e);  // 0 where m = -inf
     const float old = exp2_fast((M - ref) * kLog2e);
-    L = L * old + wave_sum(w > 0.f ? w * l : 0.f);
+    L = L * old + wave_sum(w * l);
     M = top;
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] *= old;
@@ -75,7 +76,7 @@ __global__ __launch_bounds__(kCombineWaves * 64) void state_combine_kernel(State
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] += shfl_xor(x[e], off);
   if (grp != 0) return;
-  const float inv = L > 0.f ? 1.f / L : 0.f;
+  const float inv = L == 0.f ? 0.f : 1.f / L;
   const u32x2_t o = {pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv)};
   *reinterpret_cast<u32x2_t*>(a.o + (size_t)row * D + 4 * ch) = o;
 }

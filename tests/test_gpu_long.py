@@ -159,6 +159,36 @@ def test_other_stream_and_shared_workspace():
         assert not ef.workspace_counters(ws).any()
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("Sq", [1, 40, 900])
+def test_query_that_is_not_finite(Sq, bad):
+    """Its rows are NaN, in one part and in many, and nobody else's."""
+    announce(f"query {bad} {Sq}")
+    B, Hq, H, D, S = 2, 8, 2, 128, 3000
+    q, k, v = (normal(170 + i, B, h, n, D).cuda() for i, (h, n) in
+               enumerate(((Hq, Sq), (H, S), (H, S))))
+    lists = ef.block_select(q, ef.block_summary(k), S, 12)
+    calls = (lambda v: ef.attention_blocks(q, k, v, lists),
+             lambda v: ef.attention_blocks(q, k, v, lists[..., -1:].contiguous()),
+             lambda v: ef.attention_shared_prefix(q, k[0], v[0], k, v),
+             lambda v: ef.attention_shared_prefix(q, k[0, :, :64].contiguous(),
+                                                  v[0, :, :64].contiguous(), k[:, :, :0],
+                                                  v[:, :, :0], causal=False))
+    want = [(f(v), f(v.abs())) for f in calls]
+    q[0, 3, Sq // 2, 5] = bad
+    q[1, 6, 0] = bad
+    rows = torch.zeros(B, Hq, Sq, dtype=torch.bool, device="cuda")
+    rows[0, 3, Sq // 2] = rows[1, 6, 0] = True
+    for f, (w, mag) in zip(calls, want):
+        got = f(v)
+        torch.cuda.synchronize()
+        assert torch.isnan(got[rows]).all()
+        # The 32 rows of a wave renew their references together, so a row's roundings may change:
+        # both results are within the tolerance of the exact one, twice that of each other.
+        w, mag = f64(w[~rows]), f64(mag[~rows])
+        close(got[~rows], w, 2 * mag + np.abs(w), "other rows")
+
+
 def test_other_stream_without_a_workspace():
     """A call on another stream makes what it needs there: nothing of it waits for, or is
     overtaken by, the work of the current stream."""
