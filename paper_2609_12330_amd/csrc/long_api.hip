@@ -150,7 +150,11 @@ ef_status combine_states(const Params& a, long long rows, hipStream_t stream) {
   return from_hip(ef::launch_state_combine(c, stream));
 }
 
-// Workgroups that fill the chip: two of the matrix-core kernels fit on a compute unit.
+// Workgroups that fill the chip: two of the matrix-core kernels fit on a compute unit (with
+// heads of 64 three do, but more parts mean more lists and states). 512 / 640 / 768 /
+// 1024 (us): one token over 64 blocks, 16 sequences of 32/8 heads of 128 48 / 61 / 56 / 54, 8
+// of them 29 / 40 / 37 / 36; 5 tokens over 24 blocks, 8 sequences of 64/8 heads of 64 29 /
+// 28 / 27 / 36, one token of them 16.4 / 17.7 / 18.0 / 24.0.
 constexpr long long kFillWgs = 512;
 
 // Launch shape of attention over selected blocks. The rows of a kv head are cut into
