@@ -61,6 +61,9 @@ __device__ __forceinline__ float unordered(uint32_t u) {
   return __uint_as_float(u ^ ((u >> 31) ? 0x80000000u : 0xffffffffu));
 }
 
+// ordered(-inf), the score of a block whose products are NaN; a place without a block has 0.
+constexpr uint32_t kLowest = 0x007fffffu;
+
 // LDS written by other lanes of this wave becomes visible to it.
 __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -233,8 +236,9 @@ struct Scores {
   __device__ __forceinline__ void each_key(F f) const {
     each([&](int i, float x) { f(i, has(i) ? ordered(x) : 0u); });
   }
-  // Scores from the value of `least` on (compared as floats, which cost no conversion; of
-  // -inf, where places without a block count too, and below it no use is made).
+  // Scores from the value of `least` on, compared as floats, which cost no conversion: an
+  // integer below kLowest is a NaN, from which on nothing would count, and at kLowest itself
+  // places without a block would. Neither is asked for (see bisect).
   __device__ __forceinline__ int count(uint32_t least) const {
     const float t = unordered(least);
     int k = 0;
@@ -252,7 +256,8 @@ __device__ __forceinline__ int rank_in(unsigned long long set, int n = 0) {
 // A T in [lo, hi] with count(T) = need, or the largest with count(T) >= need, by halves of
 // the interval of values, a step per bit of the answer's place among them (halving the
 // integers would first look for its exponent), then of the integers between. On entry
-// count(lo) = cnt >= need and nothing is above hi.
+// count(lo) = cnt >= need, lo is kLowest or more, and nothing is above hi; only integers
+// above lo are counted, none of which is a NaN.
 template <class F>
 __device__ __forceinline__ uint32_t bisect(uint32_t lo, uint32_t hi, int need, int& cnt, F count) {
   for (int step = 0; cnt != need && lo < hi; ++step) {
@@ -357,7 +362,7 @@ __device__ __forceinline__ bool choose(const Choice& a, lds_int* scratch) {
   // The few scores that can be in or near the border, one to a lane, in index order.
   float few = kNegInf;
   int few_block = c0 + lane, held = c1 - c0;
-  uint32_t low = 0;  // no more than the need-th largest
+  uint32_t low = kLowest;  // no more than the need-th largest
   if (held <= 64) {
     if (lane < held) few = scores.fetch(0);
     keys[lane] = few;
@@ -366,7 +371,7 @@ __device__ __forceinline__ bool choose(const Choice& a, lds_int* scratch) {
     wave_lds_sync();
     const float least = nth(best, above(keys, 64, best), need);
     wave_lds_sync();  // read before they are written again
-    if (least > kNegInf) low = ordered(least);
+    low = ordered(least);
     // (Minus an infinite bound this is -inf, or NaN: then they are not few.)
     const float base = least - fmaxf(a.apart(least), a.apart(most_of_all));
     held = 0;
@@ -418,7 +423,7 @@ __device__ __forceinline__ bool choose(const Choice& a, lds_int* scratch) {
   }
 
   // Too many for the lanes: the same on all scores, unless exact ones are called for.
-  int cnt = low ? scores.count(low) : c1 - c0;
+  int cnt = low > kLowest ? scores.count(low) : c1 - c0;
   const uint32_t T = bisect(low, top, need, cnt, [&](uint32_t t) { return scores.count(t); });
   uint32_t in = 0xffffffffu, outside = 0;
   scores.each_key([&](int, uint32_t x) {
@@ -476,7 +481,7 @@ __device__ __forceinline__ void choose_many(const Choice& a) {
   scores.each_key([&](int, uint32_t x) { top = max(top, x); });
   top = __builtin_amdgcn_readfirstlane(wave_max(top));
   int cnt = c1 - c0;
-  uint32_t T = bisect(0, top, need, cnt, [&](uint32_t t) { return scores.count(t); });
+  uint32_t T = bisect(kLowest, top, need, cnt, [&](uint32_t t) { return scores.count(t); });
   uint32_t in = 0xffffffffu, outside = 0;
   scores.each_key([&](int, uint32_t x) {
     in = min(in, x >= T ? x : 0xffffffffu);
