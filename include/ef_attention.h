@@ -424,7 +424,8 @@ ef_status ef_attention_splitkv_noalloc(const void* q, const void* k, const void*
  *     len_b = lengths[b] valid keys (clamped to [0, Skv]); Skv, the extent of its
  *     buffers, is then a capacity. With NULL every sequence has Skv keys. What lies
  *     behind a sequence's length is never read. Keys and values below it must be
- *     finite. A query that is not makes its own attention rows NaN.
+ *     finite. A query that is not makes those of its own attention rows NaN that see
+ *     a key, and no others.
  *   - Query i of sequence b sits at key n_i = i + len_b - Sq of its sequence (its
  *     queries are its last Sq positions); a negative n_i sees nothing.
  *   - o is bf16, the type the next product takes: one rounding of an fp32 result.

@@ -158,6 +158,11 @@ void attn_blocks_kernel(BlocksParams a) {
   const int first = (int)((long long)total * p / a.P);
   const int last = (int)((long long)total * (p + 1) / a.P);
   const KeyMask mask{lim, INT_MIN, 0, h};
+  auto sees = [&] {  // a listed block up to the position's own holds a key that it sees
+    bool any = false;
+    for (int e = 0; e < a.K; ++e) any |= entry(tl.pos * a.K + e) >= 0;
+    return any;
+  };
   for (int f = first; f < last; f += kWindow) {
     const int n = min(last - f, kWindow);
     __syncthreads();
@@ -186,7 +191,7 @@ void attn_blocks_kernel(BlocksParams a) {
     const int tail = __builtin_amdgcn_readfirstlane(u.block[n - 1]);
     if (per && (tail << a.shift) + 64 >= tl.cend) --tiles;
     roll_tiles<D, SEL>(tl, tiles, mt * BM + wave * 32 < a.R, Stages{sk0, sk1, sv0, sv1}, fr, row,
-                       fmaxf(a.c_abs, 1e-30f), mask, [] {});
+                       fmaxf(a.c_abs, 1e-30f), mask, [] {}, sees);
   }
   if (a.P == 1) {
     store_row<D>(row, h, valid ? a.o + orow * D : nullptr);

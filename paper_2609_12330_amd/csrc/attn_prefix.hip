@@ -138,9 +138,12 @@ void attn_prefix_kernel(PrefixParams a) {
     tl.full_lo =
         __builtin_amdgcn_readfirstlane(wave_min(valid ? mask.lim : 0x7fffffff));
   };
+  auto sees = [&] {
+    return a.causal ? mask.lim >= 0 : a.Lp + sequence_length(a.lengths, b, a.Skv) > 0;
+  };
   // The floor keeps a zero scale well defined (every visible key gets weight 1).
   roll_tiles<D, false>(tl, last - tl.first, mt * BM + wave * 32 < rows, Stages{sk0, sk1, sv0, sv1},
-                       fr, row, fmaxf(a.c_abs, 1e-30f), mask, masks);
+                       fr, row, fmaxf(a.c_abs, 1e-30f), mask, masks, sees);
   if (a.P == 1)
     store_row<D>(row, h, valid ? a.o + orow * D : nullptr);
   else
