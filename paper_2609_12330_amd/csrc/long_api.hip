@@ -88,17 +88,20 @@ ef_status ef_block_select(const void* q, const void* summary, const int* lengths
   // different banks.
   a.stride = (nb + 15) / 16 * 16 + 4;
   // Positions per workgroup: four row tiles, which share the summaries' loads and norms,
-  // where at least three of them have a position's scores to keep, the grid still fills
-  // the chip and scores are most of the work; else one tile, with more workgroups on a
-  // compute unit for the choices, and fewer positions where they do not fit. One / four
-  // tiles (us; 4096 queries of 8 kv heads of 128; G x blocks): 4 x 1024 155 / 108, 8 x 256
-  // 171 / 117, 4 x 256 69 / 62, 4 x 128 57 / 56, 2 x 128 43 / 46, 1 x 128 36 / 40; 546 of
-  // 2 x 32 heads of 64, 1 x 56 30 / 51.
+  // where the LDS has room for the scores of at least three of them, there are positions
+  // for more than one, the grid still fills the chip and scores are most of the work; else
+  // one tile, with more workgroups on a compute unit for the choices, and fewer positions
+  // where they do not fit. One / four tiles (us; 4096 queries of 8 kv heads of 128; G x
+  // blocks): 4 x 1024 155 / 108, 8 x 256 171 / 117, 4 x 256 69 / 62, 4 x 128 57 / 56, 2 x 128
+  // 43 / 46, 1 x 128 36 / 40; 546 of 2 x 32 heads of 64, 1 x 56 30 / 51. Few queries of 64
+  // sequences of 8 kv heads of 128, G x blocks: 4 x 512, 1 of them 16.2 / 18.2, 5 26.3 / 21.8;
+  // 4 x 1024, 4 of them [one tile] 29.7 / 31.3, 6 44.3 / 34.3; 2 x 512, 8 of them [one tile]
+  // 20.5 / 22.0, 9 33.0 / 24.3.
   const long long heads = (long long)B * Hkv;
   const int row = a.stride * 4, tile = a.per > 1 ? 1 : 16 / a.gp;
   a.pos = std::min(std::min(tile, std::max(1, kLaunchLds / row)), Sq);
   const int wide = std::min(4 * tile, ef::kSelectLds / row);
-  if (a.per == 1 && wide > 2 * tile && a.gp * nb >= 512 &&
+  if (a.per == 1 && wide > 2 * tile && Sq > tile && a.gp * nb >= 512 &&
       heads * ((Sq + wide - 1) / wide) >= 512)
     a.pos = wide;
   // Eight waves share the blocks of a workgroup where the grid leaves room for them.
