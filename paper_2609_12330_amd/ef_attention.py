@@ -300,6 +300,31 @@ def _stream_handle(stream) -> Optional[int]:
         return _torch().cuda.current_stream().cuda_stream
 
 
+def _new(shape, dtype, t, stream):
+    """An uninitialised tensor on t's device, in the memory of the stream the call runs on: freed,
+    it serves later work of that stream only."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=t.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=t.device)
+
+
+def _zeros(n, t, stream, cleared=None):
+    """n bytes on t's device, the first `cleared` of them (or all) 0. With a stream both the memory
+    and its clearing are that stream's."""
+    torch = _torch()
+    if stream is not None and stream.device != t.device:
+        raise ValueError(f"stream is on {stream.device}, the tensors are on {t.device}")
+    x = _new((n,), torch.uint8, t, stream)
+    if stream is None:
+        x[:cleared].zero_()
+    else:
+        with torch.cuda.stream(stream):
+            x[:cleared].zero_()
+    return x
+
+
 def _check_qkv(q, k, v):
     torch = _torch()
     bf16 = torch.bfloat16
@@ -416,17 +441,19 @@ def splitkv_partitions(Sq, Skv, T, window=0, sinks=0) -> int:
     return -(-local_runs(Sq, Skv, window, sinks)[2] // T)
 
 
-def make_workspace(q, k, partition_size=0, window=0, sinks=0):
+def make_workspace(q, k, partition_size=0, window=0, sinks=0, stream=None):
     """A zero-filled uint8 tensor on q's GPU large enough for attention_splitkv on these
     shapes (its arrival counters must start at zero; the library leaves them zero, so the
-    workspace serves later calls of any shape whose workspace fits in it)."""
+    workspace serves later calls of any shape whose workspace fits in it). Its memory and its
+    clearing belong to `stream`, or to the current one: calls on another stream have to wait
+    for that."""
     torch = _torch()
     if not q.is_cuda:
         raise TypeError("make_workspace needs GPU tensors (the workspace lives on q's device)")
     B, Hq, Sq, D = q.shape
     Hkv, Skv = k.shape[1], k.shape[2]
     n = splitkv_workspace_size(B, Hq, Hkv, Sq, Skv, D, partition_size, window, sinks)
-    return torch.zeros(max(n, 256), dtype=torch.uint8, device=q.device)
+    return _zeros(max(n, 256), q, stream)
 
 
 # Arrival-counter region at the start of every split-KV workspace (512 slots of 256 bytes);
@@ -674,16 +701,6 @@ def _call_on(t, stream, fn, *args):
         return fn(*args, _stream_handle(stream))
 
 
-def _new(shape, dtype, t, stream):
-    """An uninitialised tensor on t's device, in the memory of the stream the call runs on: freed,
-    it serves later work of that stream only."""
-    torch = _torch()
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=t.device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=t.device)
-
-
 def num_blocks(Skv: int, block_size: int = 64) -> int:
     """Blocks of a key axis of Skv keys."""
     return -(-Skv // block_size)
@@ -762,18 +779,8 @@ def _out_bf16(q, out, stream):
 
 def _state_workspace(n, q, stream=None):
     """n bytes on q's device, the arrival counters at their start zero (they stay zero from call
-    to call); None for 0 bytes. With a stream both the memory and its clearing are that
-    stream's."""
-    if n == 0:
-        return None
-    torch = _torch()
-    workspace = _new((n,), torch.uint8, q, stream)
-    if stream is None:
-        workspace[:COUNTER_REGION_BYTES].zero_()
-    else:
-        with torch.cuda.stream(stream):
-            workspace[:COUNTER_REGION_BYTES].zero_()
-    return workspace
+    to call); None for 0 bytes."""
+    return None if n == 0 else _zeros(n, q, stream, COUNTER_REGION_BYTES)
 
 
 def _own_workspace(workspace, size, sizes, q, stream):
@@ -788,12 +795,14 @@ def _own_workspace(workspace, size, sizes, q, stream):
     return workspace.data_ptr(), workspace.nbytes, workspace
 
 
-def make_blocks_workspace(q, k, topk: int, block_size: int = 64):
-    """A workspace for attention_blocks on these shapes (None where none is needed)."""
+def make_blocks_workspace(q, k, topk: int, block_size: int = 64, stream=None):
+    """A workspace for attention_blocks on these shapes (None where none is needed). Its memory
+    and the clearing of its counters belong to `stream`, or to the current one: calls on another
+    stream have to wait for that."""
     B, Hq, Sq, D = q.shape
     n = int(ef_attention_blocks_workspace_size(B, Hq, k.shape[1], Sq, k.shape[2], D, block_size,
                                                topk))
-    return _state_workspace(n, q)
+    return _state_workspace(n, q, stream)
 
 
 def attention_blocks(q, k, v, blocks, block_size: int = 64, scale: Optional[float] = None,
@@ -821,12 +830,13 @@ def attention_blocks(q, k, v, blocks, block_size: int = 64, scale: Optional[floa
     return o
 
 
-def make_shared_prefix_workspace(q, k_prefix, k):
-    """A workspace for attention_shared_prefix on these shapes (None where none is needed)."""
+def make_shared_prefix_workspace(q, k_prefix, k, stream=None):
+    """A workspace for attention_shared_prefix on these shapes (None where none is needed). Its
+    memory belongs to a stream as make_blocks_workspace's does."""
     B, Hq, Sq, D = q.shape
     n = int(ef_attention_shared_prefix_workspace_size(B, Hq, k.shape[1], Sq, k_prefix.shape[1],
                                                       k.shape[2], D))
-    return _state_workspace(n, q)
+    return _state_workspace(n, q, stream)
 
 
 def attention_shared_prefix(q, k_prefix, v_prefix, k, v, scale: Optional[float] = None,
