@@ -357,10 +357,10 @@ def _reject_qkv(q, k, v):
     raise ValueError("k and v must be [B, Hkv, Skv, D] matching q")
 
 
-def _out(q, out):
+def _out(q, out, stream):
     torch = _torch()
     if out is None:
-        return torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        return _new(q.shape, torch.float32, q, stream)
     if out.dtype != torch.float32 or out.shape != q.shape or not out.is_contiguous():
         raise ValueError("out must be a contiguous fp32 tensor shaped like q")
     _same_device(out, q, "out")
@@ -399,7 +399,7 @@ def attention_fwd(q, k, v, scale: Optional[float] = None, causal: bool = False, 
     B, Hq, Hkv, Sq, Skv, D = _check_qkv(q, k, v)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
-    o = _out(q, out)
+    o = _out(q, out, stream)
     if _local(causal, window, sinks):
         st = ef_attention_fwd_local(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), B, Hq,
                                     Hkv, Sq, Skv, D, float(scale), window, sinks,
@@ -447,7 +447,6 @@ def make_workspace(q, k, partition_size=0, window=0, sinks=0, stream=None):
     workspace serves later calls of any shape whose workspace fits in it). Its memory and its
     clearing belong to `stream`, or to the current one: calls on another stream have to wait
     for that."""
-    torch = _torch()
     if not q.is_cuda:
         raise TypeError("make_workspace needs GPU tensors (the workspace lives on q's device)")
     B, Hq, Sq, D = q.shape
@@ -489,10 +488,10 @@ def attention_splitkv(q, k, v, scale: Optional[float] = None, causal: bool = Fal
     B, Hq, Hkv, Sq, Skv, D = _check_qkv(q, k, v)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
-    o = _out(q, out)
+    o = _out(q, out, stream)
     local = _local(causal, window, sinks)
     if workspace is None:
-        workspace = make_workspace(q, k, partition_size, window, sinks)
+        workspace = make_workspace(q, k, partition_size, window, sinks, stream)
     _check_workspace(workspace, q)
     if local:
         st = ef_attention_splitkv_local(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), B,
@@ -517,7 +516,7 @@ def attention_splitkv_noalloc(q, k, v, scale: Optional[float] = None, causal: bo
     B, Hq, Hkv, Sq, Skv, D = _check_qkv(q, k, v)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
-    o = _out(q, out)
+    o = _out(q, out, stream)
     st = ef_attention_splitkv_noalloc(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), B,
                                       Hq, Hkv, Sq, Skv, D, float(scale), causal, partition_size,
                                       _stream_handle(stream))
@@ -532,7 +531,7 @@ def attention_splitkv_partials(q, k, v, scale: Optional[float] = None, causal: b
     if scale is None:
         scale = 1.0 / math.sqrt(D)
     if workspace is None:
-        workspace = make_workspace(q, k, partition_size)
+        workspace = make_workspace(q, k, partition_size, stream=stream)
     _check_workspace(workspace, q)
     st = ef_attention_splitkv_partials(q.data_ptr(), k.data_ptr(), v.data_ptr(), B, Hq, Hkv, Sq,
                                        Skv, D, float(scale), causal, partition_size,
@@ -552,7 +551,7 @@ def combine(m, l, acc, out=None, stream=None):
             raise ValueError(f"{name} must be a contiguous fp32 GPU tensor")
     if m.shape != (rows, P) or l.shape != (rows, P):
         raise ValueError("m and l must be [rows, P]")
-    o = torch.empty(rows, D, dtype=torch.float32, device=acc.device) if out is None else out
+    o = _new((rows, D), torch.float32, acc, stream) if out is None else out
     for name, t in (("m", m), ("l", l), ("out", o)):
         _same_device(t, acc, name)
     if o.dtype != torch.float32 or o.shape != (rows, D) or not o.is_contiguous():
@@ -567,15 +566,14 @@ def tune_partition_size(q, k, v, scale: Optional[float] = None, causal: bool = F
                         window: int = 0, sinks: int = 0, workspace=None, stream=None) -> int:
     """Measured best split-KV partition size for these inputs (ef_attention_splitkv_tune).
     Without a workspace, one large enough for every candidate of at least 64 keys is made."""
-    torch = _torch()
     B, Hq, Hkv, Sq, Skv, D = _check_qkv(q, k, v)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
     local = _local(causal, window, sinks)
     if workspace is None:
-        workspace = make_workspace(q, k, 64, window, sinks)
+        workspace = make_workspace(q, k, 64, window, sinks, stream)
     _check_workspace(workspace, q)
-    o = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+    o = _out(q, None, stream)
     t = ctypes.c_int(0)
     st = ef_attention_splitkv_tune(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), B, Hq,
                                    Hkv, Sq, Skv, D, float(scale), causal, window if local else 0,
@@ -606,10 +604,10 @@ def diff_attention(q1, q2, k1, k2, v, lambda_q1, lambda_k1, lambda_q2, lambda_k2
         _same_device(t, q1, name)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
-    o = _out(q1, out)
+    o = _out(q1, out, stream)
     need = int(ef_diff_attention_workspace_size(B, Hq, Hkv, Sq, Skv, D, partition_size))
     if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q1.device)
+        workspace = _new((need,), torch.uint8, q1, stream)
     if workspace is not None:
         _check_workspace(workspace, q1)
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
@@ -629,15 +627,14 @@ def attention_decode_dsplit(q, k, v, scale: Optional[float] = None, causal: bool
     """Decode through ef_attention_decode_dsplit: d_splits workgroups per key partition, each
     writing D/d_splits output channels. With one partition (partition_size >= Skv) no workspace
     is used and nothing is merged. A workspace made here is zero-filled (arrival counters)."""
-    torch = _torch()
     B, Hq, Hkv, Sq, Skv, D = _check_qkv(q, k, v)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
-    o = _out(q, out)
+    o = _out(q, out, stream)
     need = int(ef_attention_decode_dsplit_workspace_size(B, Hq, Hkv, Sq, Skv, D, d_splits,
                                                          partition_size))
     if workspace is None and need > 0:
-        workspace = torch.zeros(need, dtype=torch.uint8, device=q.device)
+        workspace = _zeros(need, q, stream)
     if workspace is not None:
         _check_workspace(workspace, q)
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()

@@ -60,3 +60,45 @@ def test_workspace_made_for_a_stream(name):
         assert torch.equal(got, want), i
         torch.cuda.synchronize()
         assert not ef.workspace_counters(ws).any()
+
+
+def diff_args(q, k):
+    vec = [normal(402 + i, D).cuda().float() / 8 for i in range(5)]
+    return (q, q.flip(1).contiguous(), k, k.flip(2).contiguous(), k, *vec, 0.5)
+
+
+OWN = {
+    "fwd": lambda q, k, x, **s: ef.attention_fwd(q, k, k, **s),
+    "splitkv": lambda q, k, x, **s: ef.attention_splitkv(q, k, k, **s),
+    "splitkv_window": lambda q, k, x, **s: ef.attention_splitkv(q, k, k, causal=True, window=2000,
+                                                                sinks=4, **s),
+    "dsplit": lambda q, k, x, **s: ef.attention_decode_dsplit(q, k, k, **s),
+    "diff": lambda q, k, x, **s: ef.diff_attention(*x, **s),
+    "partials": lambda q, k, x, **s: ef.workspace_views(
+        ef.attention_splitkv_partials(q, k, k, partition_size=256, **s), B, HQ, 1, S, D, 256)[1],
+}
+
+
+@pytest.mark.parametrize("name", OWN)
+def test_workspace_of_the_call(name):
+    """A call on another stream that is given no workspace makes it there."""
+    announce(f"own workspace on a stream: {name}")
+    call = OWN[name]
+    q, k = tensors()
+    x = diff_args(q, k)
+    want = call(q, k, x).clone()
+    n = max(ef.splitkv_workspace_size(B, HQ, H, 1, S, D, p) for p in (0, 256))
+    busy = torch.randn(4096, 4096, device="cuda")
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i in range(3):
+        dirty(n)
+        busy = occupy(busy)
+        got = call(q, k, x, stream=stream)
+        busy = occupy(busy)
+        dirty(n)  # would take the memory of a workspace freed here
+        stream.synchronize()
+        with torch.cuda.stream(stream):
+            same = torch.equal(got, want)
+        assert same, i
+        torch.cuda.synchronize()
