@@ -171,9 +171,11 @@ size_t ef_attention_splitkv_workspace_size(int B, int Hq, int Hkv, int Sq, int S
  * found with the group's arrival counter, combines that group's rows and
  * resets the counter (one kernel instead of two). Otherwise a separate combine
  * kernel follows. A counter that is not zero when the call begins (a counter
- * region never cleared) cannot tell which workgroup is last; the producer
- * then fills that group's output rows with NaN rather than combine states
- * that may be stale.
+ * region never cleared, or written over) cannot tell which workgroup is last:
+ * from P on, the producer fills that group's output rows with NaN rather than
+ * combine states that may be stale; a value of 1 .. P - 1 looks like arrivals
+ * of the call itself and leaves the rows undefined, in this call and in later
+ * ones. Clearing the region makes the workspace good again.
  * Other arguments as for ef_attention_fwd.
  */
 ef_status ef_attention_splitkv(const void* q, const void* k, const void* v, float* o,
@@ -491,8 +493,9 @@ ef_status ef_block_select(const void* q, const void* summary, const int* lengths
  *            call that uses it, left zero by every completed call. One workspace
  *            serves any number of calls of these and the split-KV entry points, in
  *            stream order; calls that overlap in time must not share one, and neither
- *            must two captured graphs that may run at the same time. Rows whose
- *            counter was not zero are filled with NaN.
+ *            must two captured graphs that may run at the same time. A counter that
+ *            was not zero is as in ef_attention_splitkv: NaN rows from the number of
+ *            the workgroups that share a row (64 at most) on, undefined ones below.
  * Work and traffic grow with the union of the lists of about 64 * Hkv / Hq neighbouring
  * queries, which is little more than one list where neighbours choose alike.
  * Errors: EF_ERR_INVALID_BLOCKS for block_size, NB or topk; others as for

@@ -301,7 +301,8 @@ __device__ __forceinline__ void combine_shared(const float* m, const float* l, c
 }
 
 // The output rows made visibly invalid, where the arrivals cannot be trusted (a counter
-// that was not zero when the launch began).
+// that was not zero when the launch began: at the number of arrivals or above it every
+// workgroup does this and none combines; below it nothing in the launch tells).
 template <int D, int NT>
 __device__ __forceinline__ void poison_rows(uint16_t* o, size_t row0, int nrows) {
   for (int i = threadIdx.x; i < nrows * D; i += NT) o[row0 * D + i] = 0x7fc0;
