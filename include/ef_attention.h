@@ -472,7 +472,8 @@ ef_status ef_block_summary(const void* k, const int* lengths, void* summary, int
  *   topk    : 1 .. EF_MAX_TOPK, at least sink_blocks + local_blocks.
  *   sink_blocks >= 0, local_blocks >= 1.
  * Errors: EF_ERR_INVALID_BLOCKS for block_size, NB, topk, sink_blocks, local_blocks;
- * others as for ef_attention_fwd.
+ * EF_ERR_INVALID_SHAPE also for more queries of one sequence than a launch takes (Hkv * Sq of
+ * 2^22 and more may be); others as for ef_attention_fwd.
  */
 ef_status ef_block_select(const void* q, const void* summary, const int* lengths, int* blocks,
                           int B, int Hq, int Hkv, int Sq, int Skv, int D, int block_size,

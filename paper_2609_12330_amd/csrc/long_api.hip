@@ -25,6 +25,11 @@ int num_blocks(int Skv, int block_size) {
 // Most bytes of LDS a launch may ask for: any list of EF_MAX_BLOCKS scores fits.
 constexpr int kLaunchLds = 64 * 1024;
 
+// A launch holds fewer than 2^32 threads. Where a call may need more it is made in several,
+// none of more than half of that.
+constexpr long long kMaxThreads = (1LL << 32) - 1;
+constexpr long long kLaunchThreads = 1LL << 31;
+
 }  // namespace
 
 extern "C" {
@@ -107,9 +112,21 @@ ef_status ef_block_select(const void* q, const void* summary, const int* lengths
   // Eight waves share the blocks of a workgroup where the grid leaves room for them.
   a.waves = heads * ((Sq + a.pos - 1) / a.pos) <= 256 ? 8 : 4;
   const long long ptiles = ((long long)Sq + a.pos - 1) / a.pos;
-  if (heads * ptiles >= (1LL << 31)) return EF_ERR_INVALID_SHAPE;
   a.ptiles = (int)ptiles;
-  return from_hip(ef::launch_block_select(a, static_cast<hipStream_t>(stream)));
+  // Sequences per launch.
+  const int most = (int)std::min<long long>(B, kLaunchThreads / (64 * a.waves) / (Hkv * ptiles));
+  if (most < 1) return EF_ERR_INVALID_SHAPE;
+  for (int b = 0; b < B; b += most) {
+    ef::SelectParams c = a;
+    c.B = std::min(most, B - b);
+    c.q += (size_t)b * Hq * Sq * D;
+    c.s += (size_t)b * Hkv * nb * D;
+    c.lengths = lengths == nullptr ? nullptr : lengths + b;
+    c.out += (size_t)b * Hkv * Sq * topk;
+    const ef_status ls = from_hip(ef::launch_block_select(c, static_cast<hipStream_t>(stream)));
+    if (ls != EF_OK) return ls;
+  }
+  return EF_OK;
 }
 
 }  // extern "C"
@@ -142,15 +159,20 @@ void set_states(Params& a, const StateLayout& w, void* workspace) {
 
 template <class Params>
 ef_status combine_states(const Params& a, long long rows, hipStream_t stream) {
-  ef::StateCombineParams c{};
-  c.m = a.ws_m;
-  c.l = a.ws_l;
-  c.acc = a.ws_acc;
-  c.o = a.o;
-  c.rows = (int)rows;
-  c.P = a.P;
-  c.D = a.D;
-  return from_hip(ef::launch_state_combine(c, stream));
+  constexpr long long most = kLaunchThreads / 64;  // rows per launch, one wave each
+  for (long long r = 0; r < rows; r += most) {
+    ef::StateCombineParams c{};
+    c.m = a.ws_m + r * a.P;
+    c.l = a.ws_l + r * a.P;
+    c.acc = a.ws_acc + r * a.P * a.D;
+    c.o = a.o + r * a.D;
+    c.rows = (int)std::min(most, rows - r);
+    c.P = a.P;
+    c.D = a.D;
+    const ef_status st = from_hip(ef::launch_state_combine(c, stream));
+    if (st != EF_OK) return st;
+  }
+  return EF_OK;
 }
 
 // Workgroups that fill the chip: two of the matrix-core kernels fit on a compute unit (with
@@ -321,7 +343,7 @@ ef_status ef_attention_blocks(const void* q, const void* k, const void* v, const
   a.mtiles = p.mtiles;
   a.c_abs = std::fabs(scale) * ef::kLog2e;
   a.qflip = scale < 0.f ? 0x80008000u : 0u;
-  if ((long long)B * Hkv * p.mtiles * p.P >= (1LL << 31)) return EF_ERR_INVALID_SHAPE;
+  if ((long long)B * Hkv * p.mtiles * p.P * 2 * p.bm > kMaxThreads) return EF_ERR_INVALID_SHAPE;
   hipStream_t hs = static_cast<hipStream_t>(stream);
   st = from_hip(ef::launch_attention_blocks(a, hs));
   return st != EF_OK || p.P == 1 || p.fused ? st : combine_states(a, s.rows(), hs);
@@ -371,7 +393,7 @@ ef_status ef_attention_shared_prefix(const void* q, const void* k_prefix, const 
   a.P1 = p.P1; a.T1 = p.T1; a.mt1 = p.mt1;
   a.P2 = p.P2; a.T2 = p.T2; a.mt2 = p.mt2;
   a.P = p.P;
-  if (p.n_prefix + p.n_own >= (1LL << 31)) return EF_ERR_INVALID_SHAPE;
+  if ((p.n_prefix + p.n_own) * 2 * kPrefixRows > kMaxThreads) return EF_ERR_INVALID_SHAPE;
   a.n_prefix = (unsigned)p.n_prefix;
   a.n_own = (unsigned)p.n_own;
   a.c_abs = std::fabs(scale) * ef::kLog2e;
