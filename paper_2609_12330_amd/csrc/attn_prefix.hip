@@ -105,6 +105,7 @@ void attn_prefix_kernel(PrefixParams a) {
   const size_t own = ((size_t)bu * a.Hkv + hkv) * (size_t)a.Skv * D;
   tl.ko = packed ? tl.kp : a.k + own;
   tl.vo = packed ? tl.vp : a.v + own;
+  tl.full_lo = 0;  // until the rows' lengths are there (see `masks`)
   tl.once = packed ? a.mt1 == 1 : a.mt2 == 1 && !a.whole;
   int last;
   if (packed) {
