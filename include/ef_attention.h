@@ -496,7 +496,7 @@ ef_status ef_block_select(const void* q, const void* summary, const int* lengths
  *            stream order; calls that overlap in time must not share one, and neither
  *            must two captured graphs that may run at the same time. A counter that
  *            was not zero is as in ef_attention_splitkv: NaN rows from the number of
- *            the workgroups that share a row (64 at most) on, undefined ones below.
+ *            the workgroups that share a row (16 at most) on, undefined ones below.
  * Work and traffic grow with the union of the lists of about 64 * Hkv / Hq neighbouring
  * queries, which is little more than one list where neighbours choose alike.
  * Errors: EF_ERR_INVALID_BLOCKS for block_size, NB or topk; others as for

@@ -193,21 +193,23 @@ void attn_blocks_kernel(BlocksParams a) {
     roll_tiles<D, SEL>(tl, tiles, mt * BM + wave * 32 < a.R, Stages{sk0, sk1, sv0, sv1}, fr, row,
                        fmaxf(a.c_abs, 1e-30f), mask, [] {}, sees);
   }
-  if (a.P == 1) {
+  if (NW == 4 || a.P == 1) {  // (tiles of 128 rows are for launches that need no parts)
     store_row<D>(row, h, valid ? a.o + orow * D : nullptr);
     return;
   }
-  const bool shared = a.counters != nullptr;
-  store_state<D>(row, h, valid, a.ws_m, a.ws_l, a.ws_acc, orow * a.P + p, shared);
-  if (!shared) return;
-  // The last part of the head's rows to arrive combines them.
-  unsigned* const counter = a.counters + (size_t)bh * kCounterStride;
-  const size_t row0 = (size_t)bh * a.R;
-  const unsigned ticket = arrival_ticket(counter);
-  if (ticket >= (unsigned)a.P) poison_rows<D, NT>(a.o, row0, a.R);
-  if (ticket != (unsigned)(a.P - 1)) return;
-  combine_shared<D, NT>(a.ws_m, a.ws_l, a.ws_acc, a.o, row0, a.R, a.P);
-  if (threadIdx.x == 0) reset_counter(counter);
+  if constexpr (NW == 2) {
+    const bool shared = a.counters != nullptr;
+    store_state<D>(row, h, valid, a.ws_m, a.ws_l, a.ws_acc, orow * a.P + p, shared);
+    if (!shared) return;
+    // The last part of the head's rows to arrive combines them.
+    unsigned* const counter = a.counters + (size_t)bh * kCounterStride;
+    const size_t row0 = (size_t)bh * a.R;
+    const unsigned ticket = arrival_ticket(counter);
+    if (ticket >= (unsigned)a.P) poison_rows<D, NT>(a.o, row0, a.R);
+    if (ticket != (unsigned)(a.P - 1)) return;
+    combine_shared<D, NT>(a.ws_m, a.ws_l, a.ws_acc, a.o, row0, a.R, a.P);
+    if (threadIdx.x == 0) reset_counter(counter);
+  }
 }
 
 template <int D, int NW>

@@ -52,6 +52,11 @@ struct SelectParams {
   int stride;    // floats of a position's score row in LDS
 };
 
+// Combine inside the launch that stores the states: states of a row, and elements of rows,
+// that one round of its loads takes.
+constexpr int kSharedParts = 8;
+constexpr int kSharedElems = 512;
+
 // Attention over selected blocks (matrix-core kernel). With P > 1 the workgroups of a
 // row tile share its blocks and store partial states, m, l [rows][P] and
 // acc [rows][P][D]; with P = 1 they write o.

@@ -191,11 +191,18 @@ constexpr long long kFillWgs = 512;
 // 180 / 131, 2048 [512 workgroups of 128] 89 / 69 and 479 / 580, 1024 [256] 46.6 / 45.0
 // and 251 / 378, 512 38.8 / 38.6 and 138 / 200.
 //
-// `fused`: the last of P workgroups to store a state combines its head's rows, where
-// these states are few; otherwise a second kernel does, at 2 to 2.5 us between two
-// launches. Kernels' time alone, one / two (us; rows x P in brackets): one sequence over
-// 8, 16, 32, 64 blocks [32 to 256] 9.3 / 10.0, 10.6 / 10.7, 12.0 / 11.2, 15.9 / 14.8, 16
-// over 32 [16] 28.5 / 30.9, four tokens over 16, 64 [256, 1024] 18.3 / 15.3, 34 / 19.
+// `fused`: the last of P workgroups to store a state combines its head's rows, where one
+// round of its loads takes all states (4 rows of 128 or 8 of 64, 8 states of each), or two
+// do and each part is one block; otherwise a second kernel does. Two launches cost the host
+// 2 us more, which binds a loop of short calls (11.3 to 12.5 us a call); on the GPU the second
+// one is worth two rounds. One launch / two, us a call of calls in a row, then of calls in a
+// graph: one token of 32/8 heads of 128 over 8 blocks [P = 8] 9.3 / 11.5, 8.7 / 8.5; 8 sequences
+// of it 11.7 / 12.3, 11.1 / 11.4; 16 over 64 [4] 50.2 / 50.6, 50.0 / 50.4; 64/8 heads of 64 over 8
+// [8] 8.1 / 10.4, 7.7 / 8.5. Two rounds: one token over 16 blocks [16] 9.9 / 12.5, 9.6 / 8.6; 64/8
+// heads of 128 over 8 [8] 10.6 / 11.8, 10.1 / 9.1; where parts have more blocks, 16 sequences of
+// those over 16 [4] 21.1 / 20.2, 20.8 / 20.0. More: one token over 32, 64 blocks [32, 64] 11.8 /
+// 11.8, 15.5 / 12.9 and 11.4 / 10.2, 15.3 / 12.4; four tokens over 4, 16 [4, 16] 12.8 / 11.9, 16.0
+// / 11.8 and 12.5 / 9.4, 15.8 / 10.3.
 struct BlocksPlan {
   int bm, mtiles, P;
   bool fused;
@@ -208,8 +215,11 @@ BlocksPlan blocks_plan(const Shape& s, int nb, int topk) {
   p.mtiles = (int)((R + p.bm - 1) / p.bm);
   const long long groups = (long long)s.B * s.Hkv * p.mtiles;
   const long long most = std::max(1, std::min(std::min(nb, topk), 64));
-  p.P = (int)std::min(std::max(kFillWgs / std::max(groups, 1LL), 1LL), most);
-  p.fused = p.mtiles == 1 && R * p.P <= 256 && (long long)s.B * s.Hkv <= ef::kCounterSlots;
+  p.P = (int)std::min(std::max(kFillWgs / std::max(groups, 1LL), 1LL), most);  // 1 for 128 rows
+  const long long rounds = (R * s.D + ef::kSharedElems - 1) / ef::kSharedElems *
+                           ((p.P + ef::kSharedParts - 1) / ef::kSharedParts);
+  static_assert(kFillWgs / 2 <= ef::kCounterSlots, "a counter for every head whose P is 2 or more");
+  p.fused = p.mtiles == 1 && (rounds == 1 || (rounds == 2 && p.P == std::min(nb, topk)));
   return p;
 }
 
@@ -323,7 +333,6 @@ ef_status ef_attention_blocks(const void* q, const void* k, const void* v, const
     if (workspace == nullptr || workspace_bytes < w.bytes) return EF_ERR_WORKSPACE_TOO_SMALL;
     if (misaligned(workspace)) return EF_ERR_MISALIGNED;
     set_states(a, w, workspace);
-    // Few states: the last workgroup to store one combines its head's rows, in one launch.
     a.counters = p.fused ? static_cast<unsigned*>(workspace) : nullptr;
   }
   a.q = static_cast<const uint16_t*>(q);

@@ -233,13 +233,13 @@ __device__ __forceinline__ void store_state(const Rows<D>& rows, int h, bool val
 
 // Combine, by the workgroup that stored the last of them, of the P states of rows row0
 // .. row0 + nrows - 1 into bf16 rows: what state_combine.hip does, on device-scope
-// loads. D / 4 lanes take a row, four channels each; P <= kFusedMaxP.
+// loads. D / 4 lanes take a row, four channels each; P <= 2 kSharedParts.
 template <int D, int NT>
 __device__ __forceinline__ void combine_shared(const float* m, const float* l, const float* acc,
                                                uint16_t* o, size_t row0, int nrows, int P) {
-  constexpr int LPR = D / 4;              // lanes per row
-  constexpr int PPL = kFusedMaxP / LPR;   // states whose weights a lane forms
-  constexpr int BATCH = 8;                // value states in flight
+  constexpr int LPR = D / 4;  // lanes per row
+  static_assert(2 * kSharedParts <= LPR, "a lane for each state's weight");
+  static_assert(NT / LPR * D == kSharedElems, "the rows of a round");
   const int ch = threadIdx.x % LPR;
   // Rows are taken in whole waves: the lanes of a wave shuffle together.
   for (int r0 = 0; r0 < nrows; r0 += NT / LPR) {
@@ -249,54 +249,36 @@ __device__ __forceinline__ void combine_shared(const float* m, const float* l, c
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<float*>(acc + row0 * P * D), (short)0, nrows * P * D * 4, 0x00020000);
     const int off = ((valid ? r : 0) * P * D + 4 * ch) * 4;
-    float mv[PPL], lv[PPL];
+    const float mv = ch < P ? load_dev(m + base + ch) : kNegInf;
+    const float lv = ch < P ? load_dev(l + base + ch) : 0.f;
+    u32x4_t y[kSharedParts];
 #pragma unroll
-    for (int i = 0; i < PPL; ++i) {
-      const int p = ch + i * LPR;
-      mv[i] = p < P ? load_dev(m + base + p) : kNegInf;
-      lv[i] = p < P ? load_dev(l + base + p) : 0.f;
-    }
-    u32x4_t y[BATCH];
-#pragma unroll
-    for (int j = 0; j < BATCH; ++j) y[j] = load16_dev(rs, off + min(j, P - 1) * D * 4);
-    float M = mv[0];
-#pragma unroll
-    for (int i = 1; i < PPL; ++i) M = fmaxf(M, mv[i]);
+    for (int j = 0; j < kSharedParts; ++j) y[j] = load16_dev(rs, off + min(j, P - 1) * D * 4);
+    float M = mv;
 #pragma unroll
     for (int x = 1; x < LPR; x *= 2) M = fmaxf(M, shfl_xor(M, x));
-    const float ref = M == kNegInf ? 0.f : M;
-    float L = 0.f;
-#pragma unroll
-    for (int i = 0; i < PPL; ++i) {
-      mv[i] = exp2_fast((mv[i] - ref) * kLog2e);  // 0 where the state has no key
-      L = fmaf(mv[i], lv[i], L);
-    }
+    const float w = exp2_fast((mv - (M == kNegInf ? 0.f : M)) * kLog2e);  // 0: no key, no state
+    float L = w * lv;
 #pragma unroll
     for (int x = 1; x < LPR; x *= 2) L += shfl_xor(L, x);
     float s[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = 0; p0 < P; p0 += BATCH) {
+    for (int p0 = 0; p0 < P; p0 += kSharedParts) {
       if (p0 > 0) {
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j) y[j] = load16_dev(rs, off + min(p0 + j, P - 1) * D * 4);
+        for (int j = 0; j < kSharedParts; ++j)
+          y[j] = load16_dev(rs, off + min(p0 + j, P - 1) * D * 4);
       }
 #pragma unroll
-      for (int j = 0; j < BATCH; ++j) {
-        const int p = p0 + j;
-        float w = 0.f;
-#pragma unroll
-        for (int i = 0; i < PPL; ++i) {
-          const float x = __shfl(mv[i], p % LPR, LPR);
-          w = p / LPR == i ? x : w;
-        }
-        w = p < P ? w : 0.f;
+      for (int j = 0; j < kSharedParts; ++j) {
+        const float wp = __shfl(w, p0 + j, LPR);
 #pragma unroll
         for (int e = 0; e < 4; ++e)  // (a state without a key was not stored)
-          s[e] = w > 0.f ? fmaf(w, __uint_as_float(y[j][e]), s[e]) : s[e];
+          s[e] = wp > 0.f ? fmaf(wp, __uint_as_float(y[j][e]), s[e]) : s[e];
       }
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;  // NaN stays NaN
-    const u32x2_t w = {pack_bf16x2(s[0] * inv, s[1] * inv), pack_bf16x2(s[2] * inv, s[3] * inv)};
-    if (valid) *reinterpret_cast<u32x2_t*>(o + (row0 + r) * D + 4 * ch) = w;
+    const u32x2_t x = {pack_bf16x2(s[0] * inv, s[1] * inv), pack_bf16x2(s[2] * inv, s[3] * inv)};
+    if (valid) *reinterpret_cast<u32x2_t*>(o + (row0 + r) * D + 4 * ch) = x;
   }
 }
 
