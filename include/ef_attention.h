@@ -464,9 +464,9 @@ ef_status ef_block_summary(const void* k, const int* lengths, void* summary, int
  *     ties to the lower index; a NaN product counts as -inf.
  * The choice is that of exact arithmetic: where two scores are too close for fp32
  * to tell apart they are formed again in 64 bits. (Scores beyond the fp32 range
- * are outside the contract.) The result does not depend on scheduling. A summary
- * at or behind a query's local blocks is not read, so a partial last block's does
- * not matter.
+ * are outside the contract.) The result does not depend on scheduling. What a
+ * summary at or behind a query's local blocks holds does not matter, a partial last
+ * block's least of all.
  *   q       : [B][Hq][Sq][D] bf16;  summary : [B][Hkv][NB][D] bf16, NB of Skv keys.
  *   blocks  : [B][Hkv][Sq][topk] int32: ascending block indices, then -1.
  *   topk    : 1 .. EF_MAX_TOPK, at least sink_blocks + local_blocks.
@@ -516,7 +516,9 @@ size_t ef_attention_blocks_workspace_size(int B, int Hq, int Hkv, int Sq, int Sk
  * of the prefix, the same for all sequences, followed by its len_b own ones. With
  * causal != 0 query i sees the keys up to its own place, Lp + n_i, of this
  * concatenation (a place before its first key: none, and the row is 0); otherwise it
- * sees them all. Each prefix key is read once for the rows of all sequences.
+ * sees them all. A prefix key is read once for every 128 rows (Hq/Hkv * Sq of each
+ * sequence) of all sequences, instead of once per sequence; where a sequence's own rows
+ * fill such tiles and the batch's the chip, once for every 128 of a sequence's rows.
  *   k_prefix, v_prefix : [Hkv][Lp][D] bf16;  k, v : [B][Hkv][Skv][D] bf16.
  *   o         : [B][Hq][Sq][D] bf16.
  *   Lp, Skv   : either may be 0.

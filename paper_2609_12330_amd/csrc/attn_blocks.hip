@@ -15,10 +15,12 @@
 //
 // What bounds it: one token over 64 blocks of 64 keys, 16 sequences of 32/8 heads of 128
 // (267 MB), 48 us, 5.5 TB/s: HBM, less the 3.5 us in which a workgroup makes its list. 4096
-// queries over 16 blocks each of 512 (67 GFLOP) 128 us: the union of 32 positions' lists
-// is 1.65 times one list, and the matrix cores are at the rate of plain prefills on it
-// (0.86 PFLOP/s). One token of one sequence over 16 blocks 10 us: launch, the list, one
-// tile's loads, and the combine by the last workgroup (3 us). Tried and not kept: waves
+// queries over 16 blocks each of 512 (67 GFLOP) 127 to 132 us: the union of 32 positions'
+// lists is 1.65 times one list, and about 30 us do not grow with it (with 26, 52 and 104
+// blocks in every union 132, 230 and 419 us, the last 1.07 PFLOP/s): the starts and ends of
+// two rounds of workgroups. Keys that lie in L2 save 6%. One token of one sequence over 16
+// blocks 9.8 us: launch, the list, one tile's loads, and the combine by the last workgroup (3
+// us). Tried and not kept: waves
 // that pass over tiles none of their rows selected (131 -> 147 us; lists that share
 // nothing 580 -> 520); the list from ranks of entries held in registers (3400 -> 2350
 // cycles, but the walk slowed with it).

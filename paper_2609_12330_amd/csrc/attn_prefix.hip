@@ -15,12 +15,13 @@
 // writes the finished rows.
 //
 // What bounds it: with one token each, 64 sequences of 32/8 heads of 128, 32768 prefix
-// keys and 64 to 2048 own ones (412 MB, 35 GFLOP) 97 us, 4.3 TB/s: two workgroups fit on
+// keys and 64 to 2048 own ones (412 MB, 35 GFLOP) 97 us, 4.3 TB/s, and 5 the combine: two workgroups fit on
 // a compute unit (LDS, registers), 64 KiB of loads in flight between them, and a step
 // takes as long as its loads, 2.1 to 2.6 us; the prefix alone takes 52 us, the own keys
 // alone 63 (long ones of equal length run at 6.2 TB/s). Prompts of 384 tokens of 16
-// sequences behind 8192 keys (844 GFLOP) 732-750 us, 1.15 PFLOP/s: the power limit, as
-// for plain prefills. Tried and not kept: 256 rows to a workgroup of eight waves, which
+// sequences behind 8192 keys (844 GFLOP) 740-766 us, 1.10 to 1.14 PFLOP/s: the power limit,
+// as for plain prefills. A few to about 100 tokens, whose rows do not fill their tiles or
+// whose tiles do not fill the chip twice, run at 0.6 to 0.7 (see long_api.hip). Tried and not kept: 256 rows to a workgroup of eight waves, which
 // leaves one on a compute unit (99 -> 122 us); the own keys of up to four rows on the
 // vector ALU (98); the combine in the same launch (4 sequences over 2011 keys 13.6 ->
 // 14.7).

@@ -28,11 +28,12 @@
 // LDS.
 //
 // What bounds it: 4096 queries of 32/8 heads of 128, 16 of up to 1024 blocks (33 GFLOP),
-// 100 us, 62 of them the scores and 38 the choice (10 of these the exact scores, which
+// 98 us, 53 without the choice and 65 with made-up scores (10 of them the exact scores, which
 // about 1% of the positions need): instructions, with two waves on a SIMD; the matrix
 // cores are 12% busy. Two positions chosen step by step together need so many registers
-// that it takes longer. One token of 16 sequences, 32 of 1024 blocks (25 MB), 11.5 us:
-// launch, the summaries' loads, and one wave's choice, one after the other.
+// that it takes longer. One token of 16 sequences, 32 of 1024 blocks (25 MB), 11 us: launch,
+// the summaries' loads, and one wave's choice, one after the other. 777 queries of 2 x 8/4
+// heads of 64, 12 of 157 blocks, 13.1 us: two choices in a row by each wave.
 #include "ef_device.hpp"
 #include "ef_long.hpp"
 #include "wave_ops.hpp"

@@ -254,7 +254,8 @@ PrefixPlan prefix_plan(const Shape& s, int Lp) {
   p.mt2 = (int)((R + kPrefixRows - 1) / kPrefixRows);
   // `whole` spares the states and their combine, which take a row about as long as 32
   // tiles do, but walks the prefix for the empty rows of its tiles too, and needs rows
-  // for the chip. Split / whole (us; 32/8 heads of 128; sequences x tokens, prefix + 256 or
+  // for the chip (192 workgroups of the 512 that fit, 0.62 PFLOP/s, are where it begins to be
+  // the shorter one). Split / whole (us; 32/8 heads of 128; sequences x tokens, prefix + 256 or
   // 1024 keys): 24 x 32 over 2048 62 / 49, over 16384 343 / 330; 16 x 32 over 2048 42 / 46,
   // over 16384 191 / 301; 64 x 64 over 2048 258 / 163; with half of the rows empty 64 x 16
   // over 2048 73 / 65, over 16384 392 / 485, 32 x 16 over 2048 42 / 45; 16 x 100 over 700
@@ -267,9 +268,11 @@ PrefixPlan prefix_plan(const Shape& s, int Lp) {
     p.n_own = heads * p.mt2;
     return p;
   }
-  // Workgroups of the prefix: one to a compute unit keeps the matrix cores busy; half as
-  // many where the own keys have most of the work, which then get three of four places;
-  // two where the prefix is nearly all and long. 256 / 128 workgroups (us; 32/8 heads of
+  // Workgroups of the prefix: one to a compute unit; half as many where the own keys have
+  // most of the work, which then get three of four places; two where the prefix is nearly
+  // all, long and read by one row tile. (With more row tiles two were not measured; one, at
+  // one wave to a SIMD, leaves the matrix cores at 0.60 to 0.72 PFLOP/s: 24 x 16 tokens over
+  // 16384 keys 173 us, 64 x 16 392.) 256 / 128 workgroups (us; 32/8 heads of
   // 128, own keys half of the capacity in the mean; the prefix's part of the tiles in
   // brackets): 64 sequences, 32768 + 2048 keys [0.33] 106 / 98, 16384 + 1024 [0.33] 57.7 /
   // 54.9, 32 of them [0.33] 41 / 35, 16 [0.5] 27.2 / 28.0, 8 [0.67] 19.6 / 26.1, 64 over
