@@ -56,9 +56,7 @@ __device__ __forceinline__ unsigned arrival_ticket(unsigned* counter) {
 // ticket at or past the arrival count means the counter was not zero when the
 // launch began (a workspace whose counter region was never cleared), so the
 // group's combine cannot be trusted: its rows are made visibly invalid rather
-// than silently stale. (From a counter at the arrival count or above every
-// workgroup does this and none combines; a smaller one looks like arrivals of
-// the launch itself, and one of them may combine too.)
+// than silently stale.
 template <int D, int DW, int NT>
 __device__ __forceinline__ void poison_group(float* o, size_t row0, int nrows, int d0) {
   for (int i = threadIdx.x; i < nrows * DW; i += NT)
