@@ -74,8 +74,11 @@ typedef enum {
   EF_ERR_INVALID_DIFF = 11,        /* differential attention: lambda_init or eps not finite, or eps < 0 */
   EF_ERR_INVALID_SPLIT = 12,       /* d_splits not 1, 2 or 4, or more than 8 query rows per kv head */
   EF_ERR_SCRATCH_TOO_SMALL = 13,   /* the problem needs more than EF_STATIC_SCRATCH_BYTES of scratch */
-  EF_ERR_INVALID_BLOCKS = 14       /* block_size not 64 or 128, more than EF_MAX_BLOCKS blocks, or topk,
+  EF_ERR_INVALID_BLOCKS = 14,      /* block_size not 64 or 128, more than EF_MAX_BLOCKS blocks, or topk,
                                       sink_blocks, local_blocks or new_keys out of range */
+  EF_ERR_INVALID_PAGES = 15,       /* page not 16, 32, 64, 128 or 256, fewer than one page, a table width
+                                      out of range, or an unknown cache format */
+  EF_ERR_INVALID_ROPE = 16         /* rot not a multiple of 16 in 16 .. D, or an amplitude not finite */
 } ef_status;
 
 /* Version of this ABI (EF_ABI_VERSION). */
@@ -535,6 +538,130 @@ ef_status ef_attention_shared_prefix(const void* q, const void* k_prefix, const 
 /* Workspace bytes of ef_attention_shared_prefix; 0 for invalid arguments too. */
 size_t ef_attention_shared_prefix_workspace_size(int B, int Hq, int Hkv, int Sq, int Lp, int Skv,
                                                  int D);
+
+/*
+ * Serving: rotary positions, a paged key-value cache, packed sequences
+ *
+ * What a serving loop does around its matrix products: rotate the queries and keys of new
+ * tokens, append keys and values to a cache in pages, attend to the cache (one or a few new
+ * tokens of each sequence) or to packed rows (prompts, or chunks of them). Conventions as at
+ * the top of this file, but for these:
+ *   - Packed rows [T][H][D]: the rows of sequence b are starts[b] .. starts[b + 1] - 1.
+ *     starts is a device buffer of B + 1 ascending int32. Rows in front of the first sequence or
+ *     behind the last one belong to none: outputs there are left as they were. Starts out of
+ *     [0, T] count as clamped to it.
+ *   - The new tokens of a sequence are the last ones of its keys: with n_b new tokens and
+ *     len_b = lengths[b] keys, new token i stands at position len_b - n_b + i.
+ *   - A cache holds k and v, each [pages][Hkv][page][D]: bf16 (EF_CACHE_BF16), or e4m3 codes
+ *     (EF_CACHE_E4M3) beside an fp32 scale for each row, [pages][Hkv][page]. Row at of
+ *     page table[b][n] is position n * page + at of sequence b; table is a device buffer
+ *     [B][width] of int32. Entries behind a sequence's last page are not read. page is 16, 32,
+ *     64, 128 or 256.
+ *   - An entry outside 0 .. pages - 1 names no page: a token that belongs there is not written,
+ *     is read as NaN, and makes the attention rows that see it NaN.
+ *   - Caches may have any size (offsets of 64 bits). Keys and values that a row may see must be
+ *     finite, and so must the fp32 sums over them; a query that is not makes its own rows NaN
+ *     that see a key.
+ */
+#define EF_CACHE_BF16 0
+#define EF_CACHE_E4M3 1
+
+/*
+ * Rotary positions: of every row x[t][h] the pairs (a, b) among its first `rot` elements are
+ * turned by the angle 2 pi positions[t] turns[i] of pair i and multiplied by amplitude,
+ *   y_a = amplitude (x_a cos - x_b sin),  y_b = amplitude (x_b cos + x_a sin);
+ * the others are copied. Pair i is (2 i, 2 i + 1) with interleaved != 0, else (i, i + rot / 2).
+ * transpose != 0 applies the transposed map (the angle negated), which takes the gradient of y
+ * to the gradient of x.
+ *   x, out    : [T][H][D] bf16; they may be the same buffer, but not overlap otherwise.
+ *   positions : [T] int32, any value.
+ *   turns     : [rot / 2] double, device, 16-byte aligned: turns (of 2 pi) per position. Angles are formed in 64
+ *               bits, so far positions lose nothing; amplitude cos and amplitude sin are
+ *               rounded to fp32, and so is each product and sum, and the result to bf16.
+ *   rot       : a multiple of 16, 16 .. D.
+ * Errors: EF_ERR_INVALID_ROPE; others as for ef_attention_fwd.
+ */
+ef_status ef_rope(const void* x, const int* positions, const double* turns, void* out, int T,
+                  int H, int D, int rot, int interleaved, double amplitude, int transpose,
+                  void* stream);
+
+/*
+ * Appends the new tokens of every sequence to a cache: k[t] rotated and v[t] go to the row of
+ * the token's position, and with q the rotated queries to q_out, in one launch.
+ *   k, v     : [T][Hkv][D] bf16;  q, q_out : [T][Hq][D] bf16, q_out may be q; or both NULL (Hq
+ *              is then 0 or a multiple of Hkv).
+ *   turns    : as for ef_rope, or NULL: nothing is rotated (rot, interleaved and amplitude are
+ *              ignored).
+ *   lengths  : [B] int32, device: the keys of every sequence, its new tokens among them.
+ *   starts   : [B + 1] int32, or NULL: every sequence has T / B new tokens (T % B == 0).
+ *   k_scale, v_scale : [pages][Hkv][page] fp32 with EF_CACHE_E4M3 (ignored otherwise).
+ * A row of 8 bits is held as codes x / s, rounded to e4m3 once; s is the smallest power of two,
+ * at least 2^-100, that brings the row's largest finite magnitude to 448 at most. Elements that
+ * are not finite become NaN. A token in front of position 0 or behind the table is not written.
+ * Two tokens must not have the same row of the cache.
+ */
+ef_status ef_cache_write(const void* k, const void* v, const void* q, const double* turns,
+                         void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                         const int* table, const int* lengths, const int* starts, void* q_out,
+                         int T, int B, int Hq, int Hkv, int D, int pages, int page, int width,
+                         int format, int rot, int interleaved, double amplitude, void* stream);
+
+/*
+ * The cached keys and values of every sequence as packed bf16 rows: position i of sequence b
+ * goes to row starts[b] + i, starts[b + 1] - starts[b] of them (at most width * page; further
+ * rows are NaN, as those of entries that name no page). bf16 rows are copied; 8-bit ones
+ * are code times scale, which is exact for scales that ef_cache_write makes.
+ *   k_out, v_out : [T][Hkv][D] bf16.
+ */
+ef_status ef_cache_read(const void* k_cache, const void* v_cache, const float* k_scale,
+                        const float* v_scale, const int* table, const int* starts, void* k_out,
+                        void* v_out, int T, int B, int Hkv, int D, int pages, int page, int width,
+                        int format, void* stream);
+
+/*
+ * Attention of new tokens over a paged cache that holds them: row (t, hq) of new token i of
+ * sequence b sees the positions up to its own, len_b - n_b + i. A row that sees none is 0.
+ *   q, o      : [T][Hq][D] bf16.
+ *   lengths   : [B] int32, clamped to [0, width * page].
+ *   starts    : [B + 1] int32, or NULL: every sequence has T / B new tokens (T % B == 0).
+ *   max_queries : most new tokens of a sequence; of one that has more, only the first
+ *               max_queries rows are written. With starts = NULL at least T / B.
+ *   workspace : ef_attention_paged_workspace_size(...) bytes, 16-byte aligned, with the
+ *               counter region of ef_attention_splitkv's workspace at its start; the same rules.
+ *               Its size does not depend on lengths.
+ * The keys of all sequences are dealt evenly to the compute units, whatever their lengths.
+ * Results depend on how they are dealt, that is on the other sequences of the call, in the last
+ * bits; the same call gives the same bits.
+ */
+ef_status ef_attention_paged(const void* q, const void* k_cache, const void* v_cache,
+                             const float* k_scale, const float* v_scale, const int* table,
+                             const int* lengths, const int* starts, void* o, int T, int B, int Hq,
+                             int Hkv, int D, int max_queries, int pages, int page, int width,
+                             int format, float scale, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+/* Workspace bytes of ef_attention_paged; 0 for invalid arguments too. */
+size_t ef_attention_paged_workspace_size(int T, int B, int Hq, int Hkv, int D, int max_queries);
+
+/*
+ * Attention of packed sequences of any lengths: row (t, hq) of token i of sequence b over that
+ * sequence's packed keys. With causal != 0 it sees key j iff j <= i + len_b - n_b (n_b tokens,
+ * len_b keys: a prompt where they are equal, a chunk behind earlier keys otherwise), else all.
+ * A row that sees no key is 0.
+ *   q, o     : [T][Hq][D] bf16;  k, v : [Tk][Hkv][D] bf16.
+ *   starts   : [B + 1] int32, the sequences' rows of q.
+ *   k_starts : [B + 1] int32, their rows of k and v.
+ *   workspace : ef_attention_packed_workspace_size(...) bytes, 16-byte aligned (may be NULL where
+ *              that is 0). It holds partial states where few rows have many keys; calls that
+ *              overlap in time must not share one.
+ */
+ef_status ef_attention_packed(const void* q, const void* k, const void* v, const int* starts,
+                              const int* k_starts, void* o, int T, int Tk, int B, int Hq, int Hkv,
+                              int D, float scale, int causal, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of ef_attention_packed; 0 for invalid arguments too. */
+size_t ef_attention_packed_workspace_size(int T, int Tk, int B, int Hq, int Hkv, int D);
 
 #ifdef __cplusplus
 }

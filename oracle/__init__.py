@@ -26,3 +26,11 @@ from .blocks import (  # noqa: F401
     block_summary_ref,
     shared_prefix_ref,
 )
+from .serving import (  # noqa: F401
+    cached_rows,
+    packed_attention_ref,
+    paged_attention_ref,
+    rope_ref,
+    sequence_attention_ref,
+    token_places,
+)

@@ -1,0 +1,340 @@
+// Host side of the serving entry points of include/ef_attention.h: argument validation,
+// launch shapes and workspace arithmetic.
+#include <algorithm>
+#include <cmath>
+
+#include "ef_attention.h"
+#include "ef_device.hpp"
+#include "ef_serve.hpp"
+#include "host_checks.hpp"
+
+namespace {
+
+using namespace ef::host;
+
+// A launch holds fewer than 2^32 threads; these stay well below.
+constexpr long long kMaxGroups = (1LL << 31) / 256;
+
+bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+
+ef_status check_heads(int T, int B, int Hq, int Hkv, int D) {
+  if (T < 0 || B < 0 || Hq < 1 || Hkv < 1) return EF_ERR_INVALID_SHAPE;
+  if (Hq % Hkv != 0) return EF_ERR_GQA_RATIO;
+  if (D != 64 && D != 128) return EF_ERR_UNSUPPORTED_HEAD_DIM;
+  // Rows of a kv head and byte offsets inside a 64-row tile stay below 2^31.
+  if (Hkv > kMaxGridYZ || B > (1 << 30) || (long long)T * (Hq / Hkv) >= (1LL << 31) - 128)
+    return EF_ERR_INVALID_SHAPE;
+  return EF_OK;
+}
+
+// With starts = NULL every sequence has T / B tokens.
+bool uneven(const int* starts, int T, int B) { return starts == nullptr && T % B != 0; }
+
+ef_status check_pages(int pages, int page, int width, int format) {
+  if (pages < 1 || width < 0 || (format != EF_CACHE_BF16 && format != EF_CACHE_E4M3) ||
+      (page != 16 && page != 32 && page != 64 && page != 128 && page != 256) ||
+      (long long)width * page >= (1LL << 31))
+    return EF_ERR_INVALID_PAGES;
+  return EF_OK;
+}
+
+ef_status check_rope(int rot, int D, double amplitude) {
+  return rot >= 16 && rot <= D && rot % 16 == 0 && std::isfinite(amplitude)
+             ? EF_OK
+             : EF_ERR_INVALID_ROPE;
+}
+
+ef_status set_pages(ef::PagesParams& c, const void* k, const void* v, const float* ks,
+                    const float* vs, const int* table, int pages, int page, int width,
+                    int format) {
+  if (k == nullptr || v == nullptr || (width > 0 && table == nullptr)) return EF_ERR_NULL_POINTER;
+  if (format == EF_CACHE_E4M3 && (ks == nullptr || vs == nullptr)) return EF_ERR_NULL_POINTER;
+  if (misaligned(k) || misaligned(v) || misaligned4(table)) return EF_ERR_MISALIGNED;
+  if (format == EF_CACHE_E4M3 && (misaligned(ks) || misaligned(vs))) return EF_ERR_MISALIGNED;
+  c.k = static_cast<char*>(const_cast<void*>(k));
+  c.v = static_cast<char*>(const_cast<void*>(v));
+  c.k_scale = const_cast<float*>(ks);
+  c.v_scale = const_cast<float*>(vs);
+  c.table = table;
+  c.pages = pages;
+  c.width = width;
+  c.shift = 4;
+  while (1 << c.shift < page) ++c.shift;
+  return EF_OK;
+}
+
+// Tokens to a workgroup, and workgroups to these tokens' rows. Cosines and sines are formed once
+// a workgroup, so it takes four tokens with all their rows where that fills the chip eight times,
+// and one token with fewer rows each otherwise.
+ef_status run_rows(ef::RowsParams& a, bool e4m3, void* stream) {
+  const int rows = a.Hq + 2 * a.Hkv, round = 256 / (a.D / 16);
+  a.per = 1;
+  while (a.per < 4 && (long long)a.T / (2 * a.per) >= 2048) a.per *= 2;
+  const int rounds = (a.per * rows + round - 1) / round;
+  a.blocks = (int)std::min<long long>(rounds, std::max<long long>(1, 1024 / std::max(a.T, 1)));
+  if (((long long)a.T + a.per - 1) / a.per * a.blocks > kMaxGroups) return EF_ERR_INVALID_SHAPE;
+  return from_hip(ef::launch_rows(a, e4m3, static_cast<hipStream_t>(stream)));
+}
+
+// Workgroups that fill the chip: two of either attention kernel fit on a compute unit.
+constexpr int kFillWgs = 512;
+
+// Launch shape of attention over pages: see PagedParams. W workgroups share the keys of each
+// (kv head, row tile): the chip's 512 places, or one to a sequence where that is more.
+struct PagedPlan {
+  int rt, mtiles, heads, W;
+  size_t parts_off, m_off, l_off, acc_off, bytes;
+};
+
+constexpr int kMostWgs = 2048;
+
+ef_status paged_plan(PagedPlan& p, int T, int B, int Hq, int Hkv, int D, int max_queries) {
+  const ef_status st = check_heads(T, B, Hq, Hkv, D);
+  if (st != EF_OK) return st;
+  if (max_queries < 0) return EF_ERR_INVALID_SHAPE;
+  const long long rows = (long long)std::min(max_queries, T) * (Hq / Hkv);
+  p.rt = rows <= 16 ? 1 : 2;
+  const long long tile = 16 * p.rt, mtiles = (rows + tile - 1) / tile;
+  if (mtiles * Hkv > kMaxGroups) return EF_ERR_INVALID_SHAPE;
+  p.mtiles = (int)mtiles;
+  p.heads = (int)mtiles * Hkv;
+  if (p.heads == 0) return EF_OK;
+  p.W = std::max(1, std::max(kFillWgs / p.heads, std::min(B, kMostWgs / p.heads)));
+  if ((long long)p.heads * p.W > kMaxGroups) return EF_ERR_INVALID_SHAPE;
+  if ((long long)B * p.heads * (tile / 4) > kMaxGroups) return EF_ERR_INVALID_SHAPE;
+  const size_t states = (size_t)p.heads * p.W * 2 * tile;
+  p.parts_off = ef::kCounterRegionBytes;
+  p.m_off = p.parts_off + ef::ws_align256((size_t)B * p.heads * sizeof(int2));
+  p.l_off = p.m_off + ef::ws_align256(states * sizeof(float));
+  p.acc_off = p.l_off + ef::ws_align256(states * sizeof(float));
+  p.bytes = p.acc_off + states * D * sizeof(float);
+  return EF_OK;
+}
+
+// Launch shape of attention of packed sequences: see PackedParams. Row tiles of a kv head are at
+// most G T / 128 + B, and their keys are cut into parts of at least kLeastTiles tiles.
+constexpr int kLeastTiles = 8;
+
+struct PackedPlan {
+  int fill, slots, per_head;
+  size_t m_off, l_off, acc_off, bytes;
+};
+
+ef_status packed_plan(PackedPlan& p, int T, int Tk, int B, int Hq, int Hkv, int D) {
+  const ef_status st = check_heads(T, B, Hq, Hkv, D);
+  if (st != EF_OK) return st;
+  if (Tk < 0) return EF_ERR_INVALID_SHAPE;
+  constexpr long long kRows = 128;
+  const long long G = Hq / Hkv;
+  // (a sequence of one token has one tile)
+  const long long tiles = std::min(T * G / kRows + B, (long long)T * ((G + kRows - 1) / kRows));
+  p.fill = std::max(kFillWgs / Hkv, 1);
+  const long long key_tiles = ((long long)Tk + 63) / 64;
+  const long long parts = (key_tiles + kLeastTiles - 1) / kLeastTiles;
+  // A sequence of m row tiles and t > C key tiles has m ceil(t / C) < 2 m t / C units, and the
+  // sum of m t over C is at most `fill`.
+  p.slots = parts <= 1 ? 0 : (int)std::min<long long>(2LL * p.fill, tiles * parts);
+  const long long per_head = tiles + p.slots;
+  if (per_head * Hkv > kMaxGroups) return EF_ERR_INVALID_SHAPE;
+  p.per_head = (int)per_head;
+  const size_t states = (size_t)Hkv * p.slots * kRows;
+  p.m_off = 0;
+  p.l_off = ef::ws_align256(states * sizeof(float));
+  p.acc_off = 2 * p.l_off;
+  p.bytes = p.acc_off + states * D * sizeof(float);
+  return EF_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+ef_status ef_rope(const void* x, const int* positions, const double* turns, void* out, int T,
+                  int H, int D, int rot, int interleaved, double amplitude, int transpose,
+                  void* stream) {
+  ef_status st = check_heads(T, 1, H, 1, D);
+  if (st != EF_OK) return st;
+  st = check_rope(rot, D, amplitude);
+  if (st != EF_OK) return st;
+  if (T == 0) return EF_OK;
+  if (x == nullptr || positions == nullptr || turns == nullptr || out == nullptr)
+    return EF_ERR_NULL_POINTER;
+  if (misaligned(x) || misaligned(turns) || misaligned(out) || misaligned4(positions))
+    return EF_ERR_MISALIGNED;
+  ef::RowsParams a{};
+  a.q = static_cast<const uint16_t*>(x);
+  a.q_out = static_cast<uint16_t*>(out);
+  a.turns = turns;
+  a.positions = positions;
+  a.T = T; a.B = 1; a.Hq = H; a.D = D;
+  a.rot = rot;
+  a.interleaved = interleaved ? 1 : 0;
+  a.amplitude = amplitude;
+  a.transpose = transpose ? 1 : 0;
+  return run_rows(a, false, stream);
+}
+
+ef_status ef_cache_write(const void* k, const void* v, const void* q, const double* turns,
+                         void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                         const int* table, const int* lengths, const int* starts, void* q_out,
+                         int T, int B, int Hq, int Hkv, int D, int pages, int page, int width,
+                         int format, int rot, int interleaved, double amplitude, void* stream) {
+  ef_status st = check_heads(T, B, Hq == 0 ? Hkv : Hq, Hkv, D);
+  if (st != EF_OK) return st;
+  if (Hq < 0) return EF_ERR_INVALID_SHAPE;
+  st = check_pages(pages, page, width, format);
+  if (st != EF_OK) return st;
+  if (turns != nullptr) {
+    st = check_rope(rot, D, amplitude);
+    if (st != EF_OK) return st;
+  }
+  if (T == 0 || B == 0) return EF_OK;
+  if (uneven(starts, T, B)) return EF_ERR_INVALID_SHAPE;
+  if (k == nullptr || v == nullptr || lengths == nullptr || (q == nullptr) != (q_out == nullptr))
+    return EF_ERR_NULL_POINTER;
+  if (misaligned(k) || misaligned(v) || misaligned(q) || misaligned(q_out) || misaligned(turns) ||
+      misaligned4(lengths) || misaligned4(starts))
+    return EF_ERR_MISALIGNED;
+  ef::RowsParams a{};
+  st = set_pages(a.c, k_cache, v_cache, k_scale, v_scale, table, pages, page, width, format);
+  if (st != EF_OK) return st;
+  a.q = static_cast<const uint16_t*>(q);
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.turns = turns;
+  a.lengths = lengths;
+  a.starts = starts;
+  a.T = T; a.B = B; a.Hq = q == nullptr ? 0 : Hq; a.Hkv = Hkv; a.D = D;
+  a.rot = turns == nullptr ? 0 : rot;
+  a.interleaved = interleaved ? 1 : 0;
+  a.amplitude = amplitude;
+  return run_rows(a, format == EF_CACHE_E4M3, stream);
+}
+
+ef_status ef_cache_read(const void* k_cache, const void* v_cache, const float* k_scale,
+                        const float* v_scale, const int* table, const int* starts, void* k_out,
+                        void* v_out, int T, int B, int Hkv, int D, int pages, int page, int width,
+                        int format, void* stream) {
+  ef_status st = check_heads(T, B, Hkv, Hkv, D);
+  if (st != EF_OK) return st;
+  st = check_pages(pages, page, width, format);
+  if (st != EF_OK) return st;
+  if (T == 0 || B == 0) return EF_OK;
+  if (starts == nullptr || k_out == nullptr || v_out == nullptr) return EF_ERR_NULL_POINTER;
+  if (misaligned(k_out) || misaligned(v_out) || misaligned4(starts)) return EF_ERR_MISALIGNED;
+  ef::CacheReadParams a{};
+  st = set_pages(a.c, k_cache, v_cache, k_scale, v_scale, table, pages, page, width, format);
+  if (st != EF_OK) return st;
+  a.starts = starts;
+  a.k_out = static_cast<uint16_t*>(k_out);
+  a.v_out = static_cast<uint16_t*>(v_out);
+  a.T = T; a.B = B; a.Hkv = Hkv; a.D = D;
+  return from_hip(ef::launch_cache_read(a, format == EF_CACHE_E4M3,
+                                        static_cast<hipStream_t>(stream)));
+}
+
+size_t ef_attention_paged_workspace_size(int T, int B, int Hq, int Hkv, int D, int max_queries) {
+  PagedPlan p{};
+  if (paged_plan(p, T, B, Hq, Hkv, D, max_queries) != EF_OK || B == 0) return 0;
+  return p.bytes;
+}
+
+ef_status ef_attention_paged(const void* q, const void* k_cache, const void* v_cache,
+                             const float* k_scale, const float* v_scale, const int* table,
+                             const int* lengths, const int* starts, void* o, int T, int B, int Hq,
+                             int Hkv, int D, int max_queries, int pages, int page, int width,
+                             int format, float scale, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  PagedPlan p{};
+  ef_status st = paged_plan(p, T, B, Hq, Hkv, D, max_queries);
+  if (st != EF_OK) return st;
+  st = check_pages(pages, page, width, format);
+  if (st != EF_OK) return st;
+  // The units of work of a head are counted in 32 bits.
+  if ((long long)B * ((long long)width * page / 64 + 1) >= (1LL << 31)) return EF_ERR_INVALID_SHAPE;
+  if (!std::isfinite(scale)) return EF_ERR_INVALID_SCALE;
+  if (T == 0 || B == 0) return EF_OK;
+  if (uneven(starts, T, B) || (starts == nullptr && max_queries < T / B))
+    return EF_ERR_INVALID_SHAPE;
+  if (p.heads == 0) return EF_OK;  // no row of a sequence is asked for
+  if (q == nullptr || o == nullptr || lengths == nullptr) return EF_ERR_NULL_POINTER;
+  if (misaligned(q) || misaligned(o) || misaligned4(lengths) || misaligned4(starts))
+    return EF_ERR_MISALIGNED;
+  ef::PagedParams a{};
+  st = set_pages(a.c, k_cache, v_cache, k_scale, v_scale, table, pages, page, width, format);
+  if (st != EF_OK) return st;
+  if (workspace == nullptr || workspace_bytes < p.bytes) return EF_ERR_WORKSPACE_TOO_SMALL;
+  if (misaligned(workspace)) return EF_ERR_MISALIGNED;
+  char* const ws = static_cast<char*>(workspace);
+  a.q = static_cast<const uint16_t*>(q);
+  a.o = static_cast<uint16_t*>(o);
+  a.lengths = lengths;
+  a.starts = starts;
+  a.parts = reinterpret_cast<int2*>(ws + p.parts_off);
+  a.ws_m = reinterpret_cast<float*>(ws + p.m_off);
+  a.ws_l = reinterpret_cast<float*>(ws + p.l_off);
+  a.ws_acc = reinterpret_cast<float*>(ws + p.acc_off);
+  a.T = T; a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.D = D;
+  a.G = Hq / Hkv;
+  a.max_queries = max_queries;
+  a.rt = p.rt;
+  a.mtiles = p.mtiles;
+  a.heads = p.heads;
+  a.W = p.W;
+  // The floor keeps a zero scale well defined (every visible key gets weight 1).
+  a.c_abs = std::fmax(std::fabs(scale) * ef::kLog2e, 1e-30f);
+  a.qflip = scale < 0.f ? 0x80008000u : 0u;
+  return from_hip(ef::launch_attention_paged(a, format == EF_CACHE_E4M3,
+                                             static_cast<hipStream_t>(stream)));
+}
+
+size_t ef_attention_packed_workspace_size(int T, int Tk, int B, int Hq, int Hkv, int D) {
+  PackedPlan p{};
+  if (packed_plan(p, T, Tk, B, Hq, Hkv, D) != EF_OK || T == 0 || B == 0) return 0;
+  return p.bytes;
+}
+
+ef_status ef_attention_packed(const void* q, const void* k, const void* v, const int* starts,
+                              const int* k_starts, void* o, int T, int Tk, int B, int Hq, int Hkv,
+                              int D, float scale, int causal, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  PackedPlan p{};
+  const ef_status st = packed_plan(p, T, Tk, B, Hq, Hkv, D);
+  if (st != EF_OK) return st;
+  if (!std::isfinite(scale)) return EF_ERR_INVALID_SCALE;
+  if (T == 0 || B == 0) return EF_OK;
+  if (q == nullptr || o == nullptr || starts == nullptr || k_starts == nullptr ||
+      (Tk > 0 && (k == nullptr || v == nullptr)))
+    return EF_ERR_NULL_POINTER;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(o) || misaligned4(starts) ||
+      misaligned4(k_starts))
+    return EF_ERR_MISALIGNED;
+  ef::PackedParams a{};
+  if (p.slots > 0) {
+    if (workspace == nullptr || workspace_bytes < p.bytes) return EF_ERR_WORKSPACE_TOO_SMALL;
+    if (misaligned(workspace)) return EF_ERR_MISALIGNED;
+    char* const ws = static_cast<char*>(workspace);
+    a.ws_m = reinterpret_cast<float*>(ws + p.m_off);
+    a.ws_l = reinterpret_cast<float*>(ws + p.l_off);
+    a.ws_acc = reinterpret_cast<float*>(ws + p.acc_off);
+  }
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.starts = starts;
+  a.k_starts = k_starts;
+  a.o = static_cast<uint16_t*>(o);
+  a.T = T; a.Tk = Tk; a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.D = D;
+  a.G = Hq / Hkv;
+  a.causal = causal ? 1 : 0;
+  a.fill = p.fill;
+  a.least = kLeastTiles;
+  a.slots = p.slots;
+  a.per_head = p.per_head;
+  a.c_abs = std::fabs(scale) * ef::kLog2e;
+  a.qflip = scale < 0.f ? 0x80008000u : 0u;
+  return from_hip(ef::launch_attention_packed(a, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -34,6 +34,8 @@ STATUS_NAMES = {
     12: "EF_ERR_INVALID_SPLIT",
     13: "EF_ERR_SCRATCH_TOO_SMALL",
     14: "EF_ERR_INVALID_BLOCKS",
+    15: "EF_ERR_INVALID_PAGES",
+    16: "EF_ERR_INVALID_ROPE",
 }
 
 # Bytes of static scratch behind ef_attention_splitkv_noalloc (EF_STATIC_SCRATCH_BYTES).
@@ -43,8 +45,12 @@ STATIC_SCRATCH_BYTES = 32 << 20
 MAX_BLOCKS = 16000
 MAX_TOPK = 256
 
+# Formats of a paged cache (EF_CACHE_BF16, EF_CACHE_E4M3).
+CACHE_BF16, CACHE_E4M3 = 0, 1
+
 # Exported symbols and their C signatures (restype, argtypes).
 _vp, _fp, _i, _f, _sz = ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+_d = ctypes.c_double
 SIGNATURES = {
     "ef_abi_version": (_i, []),
     "ef_status_string": (ctypes.c_char_p, [_i]),
@@ -82,6 +88,13 @@ SIGNATURES = {
     "ef_attention_shared_prefix": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i,
                                         _i, _f, _i, _vp, _sz, _vp]),
     "ef_attention_shared_prefix_workspace_size": (_sz, [_i, _i, _i, _i, _i, _i, _i]),
+    "ef_rope": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _d, _i, _vp]),
+    "ef_cache_write": (_i, [_vp] * 12 + [_i] * 11 + [_d, _vp]),
+    "ef_cache_read": (_i, [_vp] * 8 + [_i] * 8 + [_vp]),
+    "ef_attention_paged": (_i, [_vp] * 9 + [_i] * 10 + [_f, _vp, _sz, _vp]),
+    "ef_attention_paged_workspace_size": (_sz, [_i, _i, _i, _i, _i, _i]),
+    "ef_attention_packed": (_i, [_vp] * 6 + [_i] * 6 + [_f, _i, _vp, _sz, _vp]),
+    "ef_attention_packed_workspace_size": (_sz, [_i, _i, _i, _i, _i, _i]),
 }
 
 
@@ -269,6 +282,47 @@ def ef_attention_shared_prefix(q, k_prefix, v_prefix, k, v, lengths, o, B, Hq, H
 
 def ef_attention_shared_prefix_workspace_size(B, Hq, Hkv, Sq, Lp, Skv, D) -> int:
     return _lib().ef_attention_shared_prefix_workspace_size(B, Hq, Hkv, Sq, Lp, Skv, D)
+
+
+def ef_rope(x, positions, turns, out, T, H, D, rot, interleaved, amplitude, transpose, stream) -> int:
+    return _lib().ef_rope(x, positions, turns, out, T, H, D, rot, int(interleaved), amplitude,
+                          int(transpose), stream)
+
+
+def ef_cache_write(k, v, q, turns, k_cache, v_cache, k_scale, v_scale, table, lengths, starts, q_out,
+                   T, B, Hq, Hkv, D, pages, page, width, format, rot, interleaved, amplitude,
+                   stream) -> int:
+    return _lib().ef_cache_write(k, v, q, turns, k_cache, v_cache, k_scale, v_scale, table, lengths,
+                                 starts, q_out, T, B, Hq, Hkv, D, pages, page, width, format, rot,
+                                 int(interleaved), amplitude, stream)
+
+
+def ef_cache_read(k_cache, v_cache, k_scale, v_scale, table, starts, k_out, v_out, T, B, Hkv, D,
+                  pages, page, width, format, stream) -> int:
+    return _lib().ef_cache_read(k_cache, v_cache, k_scale, v_scale, table, starts, k_out, v_out, T,
+                                B, Hkv, D, pages, page, width, format, stream)
+
+
+def ef_attention_paged(q, k_cache, v_cache, k_scale, v_scale, table, lengths, starts, o, T, B, Hq,
+                       Hkv, D, max_queries, pages, page, width, format, scale, workspace,
+                       workspace_bytes, stream) -> int:
+    return _lib().ef_attention_paged(q, k_cache, v_cache, k_scale, v_scale, table, lengths, starts,
+                                     o, T, B, Hq, Hkv, D, max_queries, pages, page, width, format,
+                                     scale, workspace, workspace_bytes, stream)
+
+
+def ef_attention_paged_workspace_size(T, B, Hq, Hkv, D, max_queries) -> int:
+    return _lib().ef_attention_paged_workspace_size(T, B, Hq, Hkv, D, max_queries)
+
+
+def ef_attention_packed(q, k, v, starts, k_starts, o, T, Tk, B, Hq, Hkv, D, scale, causal, workspace,
+                        workspace_bytes, stream) -> int:
+    return _lib().ef_attention_packed(q, k, v, starts, k_starts, o, T, Tk, B, Hq, Hkv, D, scale,
+                                      int(causal), workspace, workspace_bytes, stream)
+
+
+def ef_attention_packed_workspace_size(T, Tk, B, Hq, Hkv, D) -> int:
+    return _lib().ef_attention_packed_workspace_size(T, Tk, B, Hq, Hkv, D)
 
 
 # ---------------------------------------------------------------------------
@@ -860,4 +914,316 @@ def attention_shared_prefix(q, k_prefix, v_prefix, k, v, scale: Optional[float] 
                   v_prefix.data_ptr(), k.data_ptr(), v.data_ptr(), _lengths_ptr(lengths, B, q),
                   o.data_ptr(), B, Hq, Hkv, Sq, Lp, Skv, D, float(scale), causal, ptr, n)
     _check(st, "ef_attention_shared_prefix")
+    return o
+
+
+# ---------------------------------------------------------------------------
+# Serving: rotary positions, a paged key-value cache, packed sequences
+# ---------------------------------------------------------------------------
+
+
+class Rope:
+    """Rotary positions (see make_rope): `turns`, float64 [rot / 2] on the GPU, are the turns (of
+    2 pi) of each pair per position."""
+
+    __slots__ = ("turns", "rot", "interleaved", "amplitude")
+
+    def __init__(self, turns, interleaved: bool = False, amplitude: float = 1.0):
+        _check_tensor(turns, "turns", _torch().float64, 1)
+        self.turns = turns
+        self.rot = 2 * turns.shape[0]
+        self.interleaved = bool(interleaved)
+        self.amplitude = float(amplitude)
+
+
+def rope_turns(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+               length: int = 0, low: float = 1.0, high: float = 4.0):
+    """Turns per position of the rot / 2 pairs, float64 on the CPU: base^(-2 i / rot) / 2 pi, and
+    for contexts `factor` times as long as `length`, the one that was trained on:
+      "linear"  every turn divided by factor;
+      "base"    base factor^(rot / (rot - 2)) in the place of base: the slowest pair is divided by
+                factor, the fastest stays;
+      "turns"   pairs that turn `high` times or more in `length` positions stay, those that turn
+                `low` times or fewer are divided by factor, between them linear in their turns;
+      "index"   the same borders, between them linear in the pair's number."""
+    torch = _torch()
+    if rot < 2 or rot % 2:
+        raise ValueError("rot must be a positive even number")
+    if not (base > 0 and factor > 0):
+        raise ValueError("base and factor must be positive")
+    if scaling not in ("none", "linear", "base", "turns", "index"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    if scaling in ("turns", "index") and not (length > 0 and 0 < low < high):
+        raise ValueError(f"scaling {scaling!r} needs length > 0 and 0 < low < high")
+    if scaling == "base":
+        if rot < 4:
+            raise ValueError("scaling 'base' needs rot >= 4")
+        base = base * factor ** (rot / (rot - 2))
+    i = torch.arange(rot // 2, dtype=torch.float64)
+    t = base ** (-2 * i / rot) / (2 * math.pi)
+    if scaling == "linear":
+        return t / factor
+    if scaling == "turns":
+        keep = ((length * t - low) / (high - low)).clamp(0, 1)
+        return t * keep + t / factor * (1 - keep)
+    if scaling == "index":
+        if base == 1.0:
+            raise ValueError("scaling 'index' needs base != 1")
+
+        def at(turns):  # number of the pair that turns so often in `length`
+            return rot * math.log(length / (turns * 2 * math.pi)) / (2 * math.log(base))
+        first, last = max(math.floor(at(high)), 0), min(math.ceil(at(low)), rot // 2 - 1)
+        keep = 1 - ((i - first) / max(last - first, 0.001)).clamp(0, 1)
+        return t * keep + t / factor * (1 - keep)
+    return t
+
+
+def make_rope(rot: int, base: float = 10000.0, interleaved: bool = False, scaling: str = "none",
+              factor: float = 1.0, length: int = 0, low: float = 1.0, high: float = 4.0,
+              amplitude: float = 1.0, device="cuda") -> Rope:
+    """Rotary positions of the first `rot` elements of a head (a multiple of 16), pairs (2 i, 2 i +
+    1) with interleaved, else (i, i + rot / 2), turned by rope_turns' angles and multiplied by
+    `amplitude`. Made once and kept."""
+    if rot % 16:
+        raise ValueError("rot must be a multiple of 16")
+    t = rope_turns(rot, base, scaling, factor, length, low, high)
+    return Rope(t.to(device), interleaved, amplitude)
+
+
+def _ints(t, name, n, ref):
+    _check_tensor(t, name, _torch().int32, 1, ref)
+    if t.shape[0] != n:
+        raise ValueError(f"{name} must have {n} entries, got {t.shape[0]}")
+    return t.data_ptr()
+
+
+def _rows3(t, name, ref=None):
+    _check_tensor(t, name, _torch().bfloat16, 3, ref)
+    return t.shape
+
+
+def _out3(x, out, stream, name="out"):
+    if out is None:
+        return _new(x.shape, _torch().bfloat16, x, stream)
+    _check_tensor(out, name, _torch().bfloat16, 3, x)
+    if out.shape != x.shape:
+        raise ValueError(f"{name} must be {tuple(x.shape)}, got {tuple(out.shape)}")
+    return out
+
+
+def _rope_args(rope, ref):
+    if rope is None:
+        return None, 0, False, 1.0
+    if rope.turns.get_device() != ref.get_device():
+        _same_device(rope.turns, ref, "rope")
+    return rope.turns.data_ptr(), rope.rot, rope.interleaved, rope.amplitude
+
+
+def rope(x, positions, rope: Rope, transpose: bool = False, out=None, stream=None):
+    """Rows x [T, H, D] turned to their positions (int32 [T], on the GPU) through ef_rope; with
+    transpose the transposed map, which takes the gradient of the result to that of x. `out` may
+    be x."""
+    T, H, D = _rows3(x, "x")
+    p = _ints(positions, "positions", T, x)
+    turns, rot, interleaved, amplitude = _rope_args(rope, x)
+    o = _out3(x, out, stream)
+    st = _call_on(x, stream, ef_rope, x.data_ptr(), p, turns, o.data_ptr(), T, H, D, rot,
+                  interleaved, amplitude, transpose)
+    _check(st, "ef_rope")
+    return o
+
+
+class PagedCache:
+    """A key-value cache in pages: k and v [pages, Hkv, page, D], bfloat16, or float8_e4m3fn with
+    float32 scales [pages, Hkv, page] for every row of either."""
+
+    __slots__ = ("k", "v", "k_scale", "v_scale", "format", "_args")
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        torch = _torch()
+        e4m3 = k.dtype is torch.float8_e4m3fn
+        kind = torch.float8_e4m3fn if e4m3 else torch.bfloat16
+        _check_tensor(k, "k", kind, 4)
+        _check_tensor(v, "v", kind, 4, k)
+        if v.shape != k.shape:
+            raise ValueError("v must be shaped like k")
+        if (k_scale is not None, v_scale is not None) != (e4m3, e4m3):
+            raise ValueError("k_scale and v_scale belong to float8_e4m3fn caches, and only to them")
+        if e4m3:
+            for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+                _check_tensor(t, name, torch.float32, 3, k)
+                if t.shape != k.shape[:3]:
+                    raise ValueError(f"{name} must be {tuple(k.shape[:3])}, got {tuple(t.shape)}")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.format = CACHE_E4M3 if e4m3 else CACHE_BF16
+        self._args = (k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if e4m3 else None,
+                      v_scale.data_ptr() if e4m3 else None)
+
+    @property
+    def shape(self):
+        """(pages, Hkv, page, D)"""
+        return self.k.shape
+
+
+def make_cache(pages: int, Hkv: int, page: int, D: int, e4m3: bool = False, device="cuda"):
+    """An uninitialised PagedCache: rows are read only after they were written."""
+    torch = _torch()
+    kind = torch.float8_e4m3fn if e4m3 else torch.bfloat16
+    kv = [torch.empty(pages, Hkv, page, D, dtype=kind, device=device) for _ in range(2)]
+    if e4m3:
+        kv += [torch.empty(pages, Hkv, page, dtype=torch.float32, device=device) for _ in range(2)]
+    return PagedCache(*kv)
+
+
+def _table(table, ref, B=None):
+    _check_tensor(table, "table", _torch().int32, 2, ref)
+    if B is not None and table.shape[0] != B:
+        raise ValueError(f"table must have {B} rows, got {table.shape[0]}")
+    return table.shape
+
+
+def _starts_ptr(starts, T, B, ref):
+    if starts is not None:
+        return _ints(starts, "starts", B + 1, ref)
+    if B and T % B:
+        raise ValueError(f"without starts every sequence has as many rows: {T} are not {B} times "
+                         "a number")
+    return None
+
+
+def cache_write(cache: PagedCache, k, v, table, lengths, starts=None, q=None,
+                rope: Optional[Rope] = None, q_out=None, stream=None):
+    """Appends the new tokens k, v [T, Hkv, D] of B sequences to the cache through ef_cache_write,
+    rotated by `rope`; returns q [T, Hq, D] rotated beside them (None without q; q_out may be q).
+    table [B, width] int32 names the sequences' pages, lengths [B] int32 their keys, the new ones
+    among them, and starts [B + 1] int32 their rows, T / B each without it."""
+    T, H, D = _rows3(k, "k")
+    if _rows3(v, "v", k) != k.shape:
+        raise ValueError("v must be shaped like k")
+    pages, Hc, page, Dc = cache.shape
+    if (Hc, Dc) != (H, D):
+        raise ValueError(f"the cache holds rows [{Hc}, {Dc}], k has [{H}, {D}]")
+    if cache.k.get_device() != k.get_device():
+        _same_device(cache.k, k, "cache")
+    B, width = _table(table, k)
+    n = _ints(lengths, "lengths", B, k)
+    s = _starts_ptr(starts, T, B, k)
+    turns, rot, interleaved, amplitude = _rope_args(rope, k)
+    Hq, qp, op = 0, None, None
+    if q is not None:
+        Tq, Hq, Dq = _rows3(q, "q", k)
+        if (Tq, Dq) != (T, D):
+            raise ValueError(f"q must be [{T}, Hq, {D}], got {tuple(q.shape)}")
+        q_out = _out3(q, q_out, stream, "q_out")
+        qp, op = q.data_ptr(), q_out.data_ptr()
+    elif q_out is not None:
+        raise ValueError("q_out needs q")
+    st = _call_on(k, stream, ef_cache_write, k.data_ptr(), v.data_ptr(), qp, turns, *cache._args,
+                  table.data_ptr(), n, s, op, T, B, Hq, H, D, pages, page, width, cache.format,
+                  rot, interleaved, amplitude)
+    _check(st, "ef_cache_write")
+    return q_out
+
+
+def cache_read(cache: PagedCache, table, starts, total: Optional[int] = None, k_out=None,
+               v_out=None, stream=None):
+    """The first starts[b + 1] - starts[b] cached rows of every sequence as packed bf16 rows k, v
+    [total, Hkv, D], through ef_cache_read. `total` may be left out where k_out and v_out are given;
+    rows that belong to no sequence are left as they were."""
+    B, width = _table(table, cache.k)
+    s = _ints(starts, "starts", B + 1, cache.k)
+    pages, H, page, D = cache.shape
+    if total is None:
+        if k_out is None or v_out is None:
+            raise ValueError("cache_read needs total, or k_out and v_out")
+        total = k_out.shape[0]
+    outs = []
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        if t is None:
+            t = _new((total, H, D), _torch().bfloat16, cache.k, stream)
+        else:
+            _check_tensor(t, name, _torch().bfloat16, 3, cache.k)
+            if t.shape != (total, H, D):
+                raise ValueError(f"{name} must be [{total}, {H}, {D}], got {tuple(t.shape)}")
+        outs.append(t)
+    st = _call_on(cache.k, stream, ef_cache_read, *cache._args, table.data_ptr(), s,
+                  outs[0].data_ptr(), outs[1].data_ptr(), total, B, H, D, pages, page, width,
+                  cache.format)
+    _check(st, "ef_cache_read")
+    return tuple(outs)
+
+
+def make_paged_workspace(q, cache: PagedCache, B: int, max_queries: int = 1, stream=None):
+    """A workspace for attention_paged on queries shaped like q [T, Hq, D] of B sequences, whatever
+    their lengths. Its memory and the clearing of its counters belong to `stream`, or to the
+    current one: calls on another stream have to wait for that."""
+    T, Hq, D = q.shape
+    n = int(ef_attention_paged_workspace_size(T, B, Hq, cache.shape[1], D, max_queries))
+    return _state_workspace(n, q, stream)
+
+
+def attention_paged(q, cache: PagedCache, table, lengths, starts=None,
+                    max_queries: Optional[int] = None, scale: Optional[float] = None,
+                    workspace=None, out=None, stream=None):
+    """Attention of the new tokens q [T, Hq, D] of B sequences over their cached keys, their own
+    among them, through ef_attention_paged; token i of n sees the positions up to lengths[b] - n +
+    i. starts [B + 1] int32 are the sequences' rows, T / B each without it; max_queries is the
+    most rows of a sequence, needed with starts. Returns bf16 shaped like q."""
+    T, Hq, D = _rows3(q, "q")
+    pages, H, page, Dc = cache.shape
+    if Dc != D:
+        raise ValueError(f"the cache holds rows of {Dc}, q has {D}")
+    if cache.k.get_device() != q.get_device():
+        _same_device(cache.k, q, "cache")
+    B, width = _table(table, q)
+    n = _ints(lengths, "lengths", B, q)
+    s = _starts_ptr(starts, T, B, q)
+    if max_queries is None:
+        if starts is not None:
+            raise ValueError("starts need max_queries, the most rows of a sequence")
+        max_queries = T // B if B else 0
+    if scale is None:
+        scale = 1.0 / math.sqrt(D)
+    o = _out3(q, out, stream)
+    ptr, nbytes, workspace = _own_workspace(workspace, ef_attention_paged_workspace_size,
+                                            (T, B, Hq, H, D, max_queries), q, stream)
+    st = _call_on(q, stream, ef_attention_paged, q.data_ptr(), *cache._args, table.data_ptr(), n, s,
+                  o.data_ptr(), T, B, Hq, H, D, max_queries, pages, page, width, cache.format,
+                  float(scale), ptr, nbytes)
+    _check(st, "ef_attention_paged")
+    return o
+
+
+def make_packed_workspace(q, k, B: int, stream=None):
+    """A workspace for attention_packed on q [T, Hq, D] and k [Tk, Hkv, D] of B sequences (None
+    where none is needed). Its memory belongs to a stream as make_paged_workspace's does."""
+    n = int(ef_attention_packed_workspace_size(q.shape[0], k.shape[0], B, q.shape[1], k.shape[1],
+                                               q.shape[2]))
+    return _state_workspace(n, q, stream)
+
+
+def attention_packed(q, k, v, starts, k_starts=None, causal: bool = True,
+                     scale: Optional[float] = None, workspace=None, out=None, stream=None):
+    """Attention of packed sequences through ef_attention_packed: rows starts[b] .. starts[b + 1] -
+    1 of q [T, Hq, D] over rows k_starts[b] .. k_starts[b + 1] - 1 of k, v [Tk, Hkv, D] (starts,
+    where k_starts is left out), the last ones of which are the rows' own with `causal`. Returns
+    bf16 shaped like q."""
+    T, Hq, D = _rows3(q, "q")
+    Tk, H, Dk = _rows3(k, "k", q)
+    if _rows3(v, "v", q) != k.shape or Dk != D:
+        raise ValueError("k and v must be [Tk, Hkv, D] matching q")
+    _check_tensor(starts, "starts", _torch().int32, 1, q)
+    B = starts.shape[0] - 1
+    if B < 0:
+        raise ValueError("starts must have an entry more than there are sequences")
+    ks = starts.data_ptr() if k_starts is None else _ints(k_starts, "k_starts", B + 1, q)
+    if scale is None:
+        scale = 1.0 / math.sqrt(D)
+    o = _out3(q, out, stream)
+    ptr, nbytes, workspace = _own_workspace(workspace, ef_attention_packed_workspace_size,
+                                            (T, Tk, B, Hq, H, D), q, stream)
+    st = _call_on(q, stream, ef_attention_packed, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                  starts.data_ptr(), ks, o.data_ptr(), T, Tk, B, Hq, H, D, float(scale), causal,
+                  ptr, nbytes)
+    _check(st, "ef_attention_packed")
     return o
