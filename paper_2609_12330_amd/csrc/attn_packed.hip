@@ -101,7 +101,7 @@ struct Extent {
   __device__ __forceinline__ int seen(const PackedParams& a, int mt) const {
     if (!a.causal) return len;
     const int top = min(mt * kRows + kRows, n * a.G) - 1;
-    return min(max(top / a.G + len - n + 1, 0), len);
+    return min(max((int)((unsigned)top / (unsigned)a.G) + len - n + 1, 0), len);
   }
 };
 
@@ -112,7 +112,9 @@ struct Unit {
   int p, P;  // part, parts of the sequence's row tiles (fewer may have keys)
   int C;     // key tiles of a part
   int slot;  // its state, where P > 1
-  // False: nothing. The same for all waves.
+  // Workgroup `id` in the order of the launch, or with SLOTS the one that has state `id`. False:
+  // there is none. The same for all waves.
+  template <bool SLOTS>
   __device__ __forceinline__ bool find(const PackedParams& a, int id) {
     const int lane = threadIdx.x & 63;
     // Sums over the sequences.
@@ -167,8 +169,8 @@ struct Unit {
         front = wave_scan(units) - units;
       }
       const int sfront = wave_scan(split) - split;
-      const auto hit = __builtin_amdgcn_ballot_w64(
-          id - before >= front && id - before < front + units);
+      const int lo = SLOTS ? slots + sfront : before + front;
+      const auto hit = __builtin_amdgcn_ballot_w64(id >= lo && id < lo + (SLOTS ? split : units));
       if (hit) {
         at = __builtin_ctzll(hit);
         e.start = __builtin_amdgcn_readlane(x.start, at);
@@ -177,7 +179,7 @@ struct Unit {
         e.len = __builtin_amdgcn_readlane(x.len, at);
         P = max(__builtin_amdgcn_readlane(parts, at), 1);
         const int tiles = __builtin_amdgcn_readlane(m, at);
-        const int in = id - before - __builtin_amdgcn_readlane(front, at);
+        const int in = id - __builtin_amdgcn_readlane(lo, at);
         mt = tiles - 1 - in / P;
         p = in % P;
         slot = slots + __builtin_amdgcn_readlane(sfront, at) + in;
@@ -204,7 +206,7 @@ void attn_packed_kernel(PackedParams a) {
   const int h = lane >> 5, ql = lane & 31;
   const int hk = (int)(blockIdx.x % a.Hkv);
   Unit u;
-  if (!u.find(a, (int)(blockIdx.x / a.Hkv))) return;
+  if (!u.find<false>(a, (int)(blockIdx.x / a.Hkv))) return;
   const Extent& e = u.e;
   const int rows = e.n * a.G;
   const int r = u.mt * kRows + wave * 32 + ql;
@@ -250,7 +252,7 @@ __global__ __launch_bounds__(256) void packed_combine_kernel(PackedParams a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int hk = (int)(blockIdx.x % a.Hkv);
   Unit u;
-  if (!u.find(a, (int)(blockIdx.x / a.Hkv)) || u.P == 1) return;
+  if (!u.find<true>(a, (int)(blockIdx.x / a.Hkv))) return;
   const int rows = min(kRows, u.e.n * a.G - u.mt * kRows);
   const int P = u.used(a);
   const size_t slot0 = (size_t)hk * a.slots + u.slot - u.p;  // state of part 0
@@ -309,7 +311,8 @@ hipError_t launch_d(const PackedParams& a, hipStream_t stream) {
   hipLaunchKernelGGL(attn_packed_kernel<D>, grid, dim3(256), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.slots == 0) return e;
-  hipLaunchKernelGGL(packed_combine_kernel<D>, grid, dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(packed_combine_kernel<D>, dim3((unsigned)a.slots * a.Hkv), dim3(256), 0,
+                     stream, a);
   return hipGetLastError();
 }
 

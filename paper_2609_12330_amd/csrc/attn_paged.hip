@@ -29,8 +29,19 @@ namespace ef {
 namespace {
 
 constexpr int kUnit = 64;             // keys of a unit of work
+// Bytes of keys that a sequence counts beside its own: what a workgroup takes from one sequence to the
+// next (rows, table, the first loads' way, the join of its waves).
+constexpr int kExtraBytes = 128 * 1024;
 constexpr float kHeadroom = 8.f;      // base-2 headroom before the reference moves
 constexpr int kStageBytes = 8192;     // keys, and values, of a wave's step
+// A value that is the same in all lanes, for the compiler to see.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// Waits until at most N of the wave's loads are on their way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+}
+constexpr int NT = 2;                 // cache policy of loads: non-temporal
 
 typedef int v2i __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
@@ -58,32 +69,108 @@ struct Geo {
 struct Sequences {
   int base;             // first one
   int start, n, len;    // rows and keys of this lane's sequence
-  int units;            // units of work of its rows in this row tile
+  int keys;             // units that hold keys of its rows in this row tile, at least one
+  int units;            // these, and EXTRA
   int scan;             // units up to and with it, from sequence `base` on
+  template <int EXTRA>
   __device__ __forceinline__ void load(const PagedParams& a, int from, int row0, int rows) {
     base = from;
     const int b = from + (int)(threadIdx.x & 63);
-    start = n = len = units = 0;
+    start = n = len = units = keys = 0;
     if (b < a.B) {
-      start = sequence_start(a.starts, b, a.B, a.T);
-      n = min(max(sequence_start(a.starts, b + 1, a.B, a.T) - start, 0), a.T);
-      len = (int)min((long long)max(a.lengths[b], 0), (long long)a.c.width << a.c.shift);
-      if (row0 < min(n, a.max_queries) * a.G) units = max((last_key(a, row0, rows) + kUnit) / kUnit, 1);
+      // Three loads at once, whether there are starts or not.
+      const int* const p = a.starts != nullptr ? a.starts + b : a.lengths + b;
+      const int s0 = p[0], s1 = p[a.starts != nullptr ? 1 : 0], l = a.lengths[b];
+      start = a.starts != nullptr ? min(max(s0, 0), a.T) : b * a.even;
+      n = a.starts != nullptr ? max(min(max(s1, 0), a.T) - start, 0) : a.even;
+      len = min(max(l, 0), a.c.width << a.c.shift);
+      if (row0 < min(n, a.max_queries) * a.G) {
+        keys = max((last_key(a, row0, rows) + kUnit) / kUnit, 1);
+        units = keys + EXTRA;
+      }
     }
     scan = wave_scan(units);
   }
   // Last key that any of the tile's rows sees (-1: none).
   __device__ __forceinline__ int last_key(const PagedParams& a, int row0, int rows) const {
     const int top = min(row0 + rows, min(n, a.max_queries) * a.G) - 1;
-    return max(top / a.G + len - n, -1);
+    return max((int)((unsigned)top / (unsigned)a.G) + len - n, -1);
   }
 };
 
+// Parts p0 .. p1 - 1 of a row joined by one wave: the value (D / 4 lanes, four channels each, the
+// same in every group of them) and the sum against the reference M (base-2 units).
+struct Joined {
+  floatx4 x;
+  float M, L;
+};
+template <int D, int BATCH, bool SHARED, class State>
+__device__ __forceinline__ Joined join_parts(const PagedParams& a, int p0, int p1, State state) {
+  constexpr int LPS = D / 4, SPL = 64 / LPS;  // lanes of a state, states of a wave-wide load
+  const int lane = threadIdx.x & 63, grp = lane / LPS, ch = lane % LPS;
+  const __amdgpu_buffer_rsrc_t rs =
+      __builtin_amdgcn_make_buffer_rsrc(a.ws_acc, (short)0, -1, 0x00020000);
+  auto value = [&](int p) -> floatx4 {
+    const size_t at = state(p) * D + 4 * ch;
+    if constexpr (SHARED) return __builtin_bit_cast(floatx4, load16_dev(rs, (int)(at * 4)));
+    return *reinterpret_cast<const floatx4*>(a.ws_acc + at);
+  };
+  Joined j = {{0.f, 0.f, 0.f, 0.f}, kNegInf, 0.f};
+  for (; p0 < p1; p0 += 64) {
+    const int count = min(p1 - p0, 64);
+    float m = kNegInf, l = 0.f;
+    if (lane < count) {
+      m = load_dev(a.ws_m + state(p0 + lane));
+      l = load_dev(a.ws_l + state(p0 + lane));
+    }
+    floatx4 y[BATCH];
+    auto fetch = [&](int q) {
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) y[i] = value(p0 + min(q + i * SPL + grp, count - 1));
+    };
+    fetch(0);
+    const float top = fmaxf(j.M, wave_max(m));
+    const float ref = top == kNegInf ? 0.f : top;
+    const float wt = exp2_fast(m - ref);  // 0 from -inf
+    const float old = exp2_fast(j.M - ref);
+    j.L = j.L * old + wave_sum(wt * l);
+    j.M = top;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) j.x[e] *= old;
+    for (int q = 0; q < count; q += BATCH * SPL) {
+      if (q > 0) fetch(q);
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) {
+        const int s = q + i * SPL + grp;
+        const float ws = __shfl(wt, min(s, 63), 64);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) j.x[e] = s < count ? fmaf(ws, y[i][e], j.x[e]) : j.x[e];
+      }
+    }
+  }
+#pragma unroll
+  for (int off = LPS; off < 64; off *= 2)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) j.x[e] += shfl_xor(j.x[e], off);
+  return j;
+}
+template <int D>
+__device__ __forceinline__ void store_joined(const Joined& j, float inv, uint16_t* o) {
+  const int lane = threadIdx.x & 63;
+  if (lane >= D / 4) return;
+  const u32x2_t p = {pack_bf16x2(j.x[0] * inv, j.x[1] * inv),
+                     pack_bf16x2(j.x[2] * inv, j.x[3] * inv)};
+  *reinterpret_cast<u32x2_t*>(o + 4 * lane) = p;
+}
+
+// (A function beside the kernel: the host's compiler reads a kernel's body too, and does not know
+// buffers.)
 template <int D, bool E4M3, int RT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
-void attn_paged_kernel(PagedParams a) {
+__device__ __forceinline__ void attend_pages(const PagedParams& a) {
   using G = Geo<D, E4M3>;
   constexpr int ROWS = 16 * RT, KT = G::KT, DT = G::DT;
+  constexpr int LEAST = 4 * KT / kUnit;  // units of a run: a step of each wave
+  constexpr int EXTRA = kExtraBytes / (2 * kUnit * G::ROWB);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, l16 = lane & 15;
@@ -99,29 +186,30 @@ void attn_paged_kernel(PagedParams a) {
   const int row0 = mt * ROWS;
 
   __shared__ __align__(1024) char sv0[4][kStageBytes], sv1[4][kStageBytes];
-  __shared__ __align__(16) float sks[2][4][KT], svs[2][4][KT];  // scales of keys and values
+  // Scales of keys and values, objects of their own for each stage like the values', so that the
+  // compiler tells the loads into one from the reads of the other.
+  __shared__ __align__(16) float sks0[4][KT], sks1[4][KT], svs0[4][KT], svs1[4][KT];
   __shared__ float sm[4][ROWS], sl[4][ROWS];
 
   // This workgroup's run of the list.
   Sequences s;
-  s.load(a, 0, row0, ROWS);
+  s.template load<EXTRA>(a, 0, row0, ROWS);
   int total = __builtin_amdgcn_readlane(s.scan, 63);
   for (int b = 64; b < a.B; b += 64) {
-    s.load(a, b, row0, ROWS);
+    s.template load<EXTRA>(a, b, row0, ROWS);
     total += __builtin_amdgcn_readlane(s.scan, 63);
   }
-  constexpr int LEAST = 4 * KT / kUnit;  // a step of each wave
-  const int T = max((int)(((long long)total + a.W - 1) / a.W), LEAST);
+  const int T = max((int)(((unsigned)total + a.W - 1) / (unsigned)a.W), LEAST);
   int u = (int)min((long long)w * T, (long long)total);
   const int u_end = (int)min((long long)u + T, (long long)total);
   if (u >= u_end) return;
   // Its first sequence.
   int before = 0;  // units in front of the sequences of `s`
-  if (a.B > 64) s.load(a, 0, row0, ROWS);
+  if (a.B > 64) s.template load<EXTRA>(a, 0, row0, ROWS);
   auto skip = [&] {
     while (s.base + 64 < a.B && before + __builtin_amdgcn_readlane(s.scan, 63) <= u) {
       before += __builtin_amdgcn_readlane(s.scan, 63);
-      s.load(a, s.base + 64, row0, ROWS);
+      s.template load<EXTRA>(a, s.base + 64, row0, ROWS);
     }
   };
 
@@ -129,14 +217,19 @@ void attn_paged_kernel(PagedParams a) {
     skip();
     const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + s.scan > u));
     const int b = s.base + at;
-    const int units = __builtin_amdgcn_readlane(s.units, at);
-    const int first = before + __builtin_amdgcn_readlane(s.scan, at) - units;  // its first unit
+    const int units = __builtin_amdgcn_readlane(s.keys, at);
+    const int behind = before + __builtin_amdgcn_readlane(s.scan, at);  // the next one's first unit
+    const int first = behind - units - EXTRA;  // its first unit
+    if (u >= first + units) {  // nothing of its keys
+      u = min(u_end, behind);
+      continue;
+    }
     const int len = __builtin_amdgcn_readlane(s.len, at);
     const int n = __builtin_amdgcn_readlane(s.n, at);
     const int start = __builtin_amdgcn_readlane(s.start, at);
     const int nrows = min(ROWS, min(n, a.max_queries) * a.G - row0);
     const int end_seen = (row0 + nrows - 1) / a.G + len - n + 1;  // keys any row sees
-    const int k0 = (u - first) * kUnit;
+    const int k0 = uniform((u - first) * kUnit);
     const int u_next = min(u_end, first + units);
     const int k1 = min((u_next - first) * kUnit, end_seen);
 
@@ -144,39 +237,22 @@ void attn_paged_kernel(PagedParams a) {
     bf16x8_t qf[RT][D / 32];
     int lim[RT];
     size_t orow[RT];
-    bool poison[RT];
     int full = 0x7fffffff;  // last key that every row sees
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       const int r = row0 + 16 * t + l16;
       const bool valid = 16 * t + l16 < nrows;
-      const int i = valid ? r / a.G : 0, hq = valid ? r % a.G : 0;
+      const int i = valid ? (unsigned)r / (unsigned)a.G : 0, hq = valid ? r - i * a.G : 0;
       lim[t] = valid ? i + len - n : -1;
       full = min(full, valid ? lim[t] : full);
       orow[t] = ((size_t)(start + i) * a.Hq + (size_t)hk * a.G + hq) * D;
-      unsigned most = 0;
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {
         // Element order of an 8-bit key's 16-byte load: two steps' operands side by side.
         const int d = E4M3 ? 64 * (x / 2) + 16 * g + 8 * (x % 2) : 32 * x + 8 * g;
-        u32x4_t v = {0u, 0u, 0u, 0u};
-        if (valid) v = *reinterpret_cast<const u32x4_t*>(a.q + orow[t] + d) ^ a.qflip;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          most = max(most, v[e] & 0x7fffu);
-          most = max(most, v[e] >> 16 & 0x7fffu);
-        }
-        qf[t][x] = __builtin_bit_cast(bf16x8_t, v);
-      }
-      // A query that is not finite: zero here, its row NaN where it sees a key.
-      most = max(most, (unsigned)__shfl_xor((int)most, 16, 64));
-      most = max(most, (unsigned)__shfl_xor((int)most, 32, 64));
-      const bool bad = most >= 0x7f80u;
-      poison[t] = bad && lim[t] >= 0;
-      if (bad) {
-        const u32x4_t zero = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int x = 0; x < D / 32; ++x) qf[t][x] = __builtin_bit_cast(bf16x8_t, zero);
+        // (Rows that are none read row 0 of the sequence, and are zeroed below.)
+        qf[t][x] = __builtin_bit_cast(bf16x8_t,
+                                      *reinterpret_cast<const u32x4_t*>(a.q + orow[t] + d));
       }
     }
     full = wave_min(full);
@@ -194,8 +270,8 @@ void attn_paged_kernel(PagedParams a) {
 
     // This wave's steps.
     const int steps = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0;
-    const int j0 = steps * wave / 4, j1 = steps * (wave + 1) / 4;
-    int wend = min(k1, k0 + j1 * KT);  // keys it may read
+    const int j0 = uniform(steps * wave / 4), j1 = uniform(steps * (wave + 1) / 4);
+    int wend = uniform(min(k1, k0 + j1 * KT));  // keys it may read
     int bad_from = 0x7fffffff;         // first key of a page that is none
     int pv = 0, p0 = -0x10000000;      // table entries p0 .. p0 + 63, one to a lane
     const int* const table = a.c.table + (size_t)b * a.c.width;
@@ -211,45 +287,50 @@ void attn_paged_kernel(PagedParams a) {
       constexpr int S = decltype(stage)::value;
       const int kb = k0 + j * KT;
       if (((min(kb + KT, wend) - 1) >> a.c.shift) - p0 >= 64) {
-        p0 = kb >> a.c.shift;
+        p0 = uniform(kb >> a.c.shift);
         const int last = (wend - 1) >> a.c.shift;
         const bool used = p0 + lane <= last;
         pv = used ? table[p0 + lane] : 0;
-        const auto none = __builtin_amdgcn_ballot_w64(used && (unsigned)pv >= (unsigned)a.c.pages);
+        const bool bad = (unsigned)pv >= (unsigned)a.c.pages;
+        const auto none = __builtin_amdgcn_ballot_w64(bad);
         if (none) {  // the walk ends in front of it
           bad_from = (p0 + __builtin_ctzll(none)) << a.c.shift;
-          wend = min(wend, bad_from);
+          wend = uniform(min(wend, bad_from));
+          pv = bad ? 0 : pv;
         }
       }
-      if (kb >= wend) return;
+      // Each 16 keys have a buffer of their own that ends behind the last one the wave may read:
+      // rows past it are zeros (masked later), and a step past it as a whole moves nothing, but
+      // its loads count: the same number is in flight whichever way the walk goes, so that waits
+      // can leave the next step's there.
       char* const vs = S == 0 ? sv0[wave] : sv1[wave];
+      auto buffer = [&](const char* base, int t) {
+        const int key = kb + 16 * t;
+        const int rows = min(max(wend - key, 0), 16);
+        const uint64_t p = (uint64_t)(uintptr_t)base + cell_of(key) * G::ROWB;
+        const uint64_t q = (uint64_t)(unsigned)uniform((int)(p >> 32)) << 32 |
+                           (unsigned)uniform((int)p);
+        return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>((uintptr_t)q), (short)0,
+                                                 uniform(rows * G::ROWB), 0x00020000);
+      };
 #pragma unroll
       for (int t = 0; t < G::T16; ++t) {
-        // Rows past the end repeat the last one (masked later).
-        const int key = min(kb + 16 * t, (wend - 1) & ~15);
-        const int left = wend - 1 - key;
-        const size_t cell = cell_of(key);
-        const char* const kp = a.c.k + cell * G::ROWB;
-        const unsigned off = (unsigned)(min(l16, left) * G::ROWB + g * 16);
+        const __amdgpu_buffer_rsrc_t rs = buffer(a.c.k, t);
 #pragma unroll
         for (int x = 0; x < G::KL; ++x)
-          kx[S][t * G::KL + x] = __builtin_nontemporal_load(
-              reinterpret_cast<const u32x4_t*>(kp + off + 64 * x));
+          kx[S][t * G::KL + x] =
+              __builtin_amdgcn_raw_buffer_load_b128(rs, l16 * G::ROWB + g * 16 + 64 * x, 0, NT);
       }
 #pragma unroll
       for (int t = 0; t < G::T16; ++t) {
-        const int key = min(kb + 16 * t, (wend - 1) & ~15);
-        const int left = wend - 1 - key;
-        const size_t cell = cell_of(key);
-        const char* const vp = a.c.v + cell * G::ROWB;
+        const __amdgpu_buffer_rsrc_t rs = buffer(a.c.v, t);
         constexpr int N = 16 / G::RPI;  // loads of 16 rows
 #pragma unroll
         for (int x = 0; x < N; ++x) {
           const int r = x * G::RPI + lane / G::KCH;
-          const unsigned off =
-              (unsigned)(min(r, left) * G::ROWB + ((lane % G::KCH) ^ G::swz(r)) * 16);
-          __builtin_amdgcn_global_load_lds(vp + off, EF_LDS(void, vs + (t * N + x) * 1024), 16, 0,
-                                           2 /* non-temporal */);
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(
+              rs, EF_LDS(void, vs + (t * N + x) * 1024), 16,
+              r * G::ROWB + ((lane % G::KCH) ^ G::swz(r)) * 16, 0, 0, NT);
         }
       }
       if constexpr (E4M3) {
@@ -259,28 +340,62 @@ void attn_paged_kernel(PagedParams a) {
           const int page = __shfl(pv, (key >> a.c.shift) - p0, 64);
           const size_t cell = (((size_t)(unsigned)page * a.Hkv + hk) << a.c.shift) +
                               (unsigned)(key & page_mask);
-          __builtin_amdgcn_global_load_lds(a.c.k_scale + cell, EF_LDS(void, &sks[S][wave][64 * x]),
-                                           4, 0, 0);
-          __builtin_amdgcn_global_load_lds(a.c.v_scale + cell, EF_LDS(void, &svs[S][wave][64 * x]),
-                                           4, 0, 0);
+          __builtin_amdgcn_global_load_lds(a.c.k_scale + cell,
+                                           EF_LDS(void, (S == 0 ? sks0 : sks1)[wave] + 64 * x), 4, 0,
+                                           0);
+          __builtin_amdgcn_global_load_lds(a.c.v_scale + cell,
+                                           EF_LDS(void, (S == 0 ? svs0 : svs1)[wave] + 64 * x), 4, 0,
+                                           0);
         }
       }
     };
-    // Offsets of this lane's transposing reads of values.
-    int vread[DT];
-#pragma unroll
-    for (int i = 0; i < DT; ++i) {
+    // Waits for a step's loads, the next step's being the only ones behind them. (In the source:
+    // the compiler was seen to leave out the wait for one of the stages in LDS.)
+    constexpr int LOADS = 16 + (E4M3 ? 2 * (KT / 64) : 0);  // of a step
+    auto landed = [] {
+      __builtin_amdgcn_sched_barrier(0);
+      wait_loads<LOADS>();
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // This lane's transposing reads of values: 16-byte chunk c of its row, at slot c ^ swz(row).
+    // Chunks are 2 i (and the next) of bf16 rows, i of e4m3 ones, so i turns the offset by an
+    // exclusive or.
+    constexpr int SLOT = E4M3 ? 16 : 32;
+    const int r8 = l16 >> 1;
+    const int vrow = E4M3 ? 16 * (r8 >> 2) + 4 * g + (r8 & 3) : 4 * g + (l16 >> 2);
+    const int vlow = vrow * G::ROWB + 8 * (l16 & 1) + (E4M3 ? 0 : 16 * ((l16 & 3) >> 1));
+    const int vturn = 16 * G::swz(vrow);
+    // Fragment i of the 32 keys at byte `at` of a stage.
+    auto value = [&](const char* vs, int turn, int at, int i) -> bf16x8_t {
+      const char* const p = vs + vlow + ((i * SLOT) ^ turn) + at;
       if constexpr (E4M3) {
-        const int r8 = l16 >> 1, r = 16 * (r8 >> 2) + 4 * g + (r8 & 3);
-        vread[i] = r * G::ROWB + ((i ^ G::swz(r)) * 16) + 8 * (l16 & 1);
+        const v2i c = __builtin_amdgcn_ds_read_tr8_b64_v2i32(EF_LDS(v2i, p));
+        const u32x4_t f = {(uint32_t)c[0], (uint32_t)c[1], 0u, 0u};
+        return __builtin_bit_cast(bf16x8_t, f);
       } else {
-        const int r = 4 * g + (l16 >> 2);
-        vread[i] = r * G::ROWB + (((2 * i + ((l16 & 3) >> 1)) ^ G::swz(r)) * 16) + 8 * (l16 & 1);
+        const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(EF_LDS(bf16x4_t, p));
+        const bf16x4_t hi =
+            __builtin_amdgcn_ds_read_tr16_b64_v4bf16(EF_LDS(bf16x4_t, p + 16 * G::ROWB));
+        return bf16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
       }
-    }
+    };
+    // Eight e4m3 codes as bf16.
+    auto widen = [](uint32_t c0, uint32_t c1) -> bf16x8_t {
+      const uint32_t c[2] = {c0, c1};
+      u32x4_t f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        f[2 * e] = __builtin_bit_cast(uint32_t,
+                                      __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[e], 1.f, false));
+        f[2 * e + 1] = __builtin_bit_cast(
+            uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[e], 1.f, true));
+      }
+      return __builtin_bit_cast(bf16x8_t, f);
+    };
     auto compute = [&](auto stage, int j) {
       constexpr int S = decltype(stage)::value;
       const int kb = k0 + j * KT;
+      landed();
       if (kb >= wend) return;
       const char* const vs = S == 0 ? sv0[wave] : sv1[wave];
       // Scores: element i of tile t is key 16 t + 4 g + i.
@@ -295,18 +410,11 @@ void attn_paged_kernel(PagedParams a) {
           if constexpr (E4M3) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              u32x4_t c;
-#pragma unroll
-              for (int f = 0; f < 2; ++f) {
-                c[2 * f] = __builtin_bit_cast(
-                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(kv[2 * e + f], 1.f, false));
-                c[2 * f + 1] = __builtin_bit_cast(
-                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(kv[2 * e + f], 1.f, true));
-              }
+              const bf16x8_t c = widen(kv[2 * e], kv[2 * e + 1]);
 #pragma unroll
               for (int r = 0; r < RT; ++r)
-                x[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                    __builtin_bit_cast(bf16x8_t, c), qf[r][2 * y + e], x[r][t], 0, 0, 0);
+                x[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c, qf[r][2 * y + e], x[r][t], 0,
+                                                                 0, 0);
             }
           } else {
 #pragma unroll
@@ -316,7 +424,8 @@ void attn_paged_kernel(PagedParams a) {
           }
         }
         if constexpr (E4M3) {
-          const floatx4 ks = *reinterpret_cast<const floatx4*>(&sks[S][wave][16 * t + 4 * g]);
+          const floatx4 ks = *reinterpret_cast<const floatx4*>(
+              (S == 0 ? sks0 : sks1)[wave] + 16 * t + 4 * g);
 #pragma unroll
           for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -366,7 +475,8 @@ void attn_paged_kernel(PagedParams a) {
           for (int e = 0; e < 4; ++e) p[e] = exp2_fast(fmaf(x[r][t][e], a.c_abs, neg));
           sum += (p[0] + p[1]) + (p[2] + p[3]);
           if constexpr (E4M3) {
-            const floatx4 vsc = *reinterpret_cast<const floatx4*>(&svs[S][wave][16 * t + 4 * g]);
+            const floatx4 vsc = *reinterpret_cast<const floatx4*>(
+                (S == 0 ? svs0 : svs1)[wave] + 16 * t + 4 * g);
 #pragma unroll
             for (int e = 0; e < 4; ++e) p[e] *= vsc[e];
           }
@@ -375,74 +485,115 @@ void attn_paged_kernel(PagedParams a) {
         }
         lsum[r] += sum;
       }
-      // Values.
+      // Values: the fragments of BATCH products are read while the ones before are multiplied.
+      constexpr int BATCH = RT == 2 && !E4M3 ? 2 : 4, NB = DT / BATCH * G::SUBS;
+      bf16x8_t vx[2][BATCH];
+      int turn = vturn;
+      asm volatile("" : "+v"(turn));  // (offsets formed here take no registers outside)
+      auto fetch = [&](int n) {
 #pragma unroll
-      for (int y = 0; y < G::SUBS; ++y)
+        for (int i = 0; i < BATCH; ++i)
+          vx[n & 1][i] = value(vs, turn, n / (DT / BATCH) * 32 * G::ROWB,
+                               n % (DT / BATCH) * BATCH + i);
+      };
+      fetch(0);
 #pragma unroll
-        for (int i = 0; i < DT; ++i) {
-          const char* const p = vs + vread[i] + 32 * y * G::ROWB;
-          bf16x8_t vx;
+      for (int n = 0; n < NB; ++n) {
+        if (n + 1 < NB) fetch(n + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        const int y = n / (DT / BATCH);
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+          bf16x8_t f = vx[n & 1][i];
           if constexpr (E4M3) {
-            const v2i c = __builtin_amdgcn_ds_read_tr8_b64_v2i32(EF_LDS(v2i, p));
-            u32x4_t f;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              f[2 * e] = __builtin_bit_cast(
-                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)c[e], 1.f, false));
-              f[2 * e + 1] = __builtin_bit_cast(
-                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)c[e], 1.f, true));
-            }
-            vx = __builtin_bit_cast(bf16x8_t, f);
-          } else {
-            const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(EF_LDS(bf16x4_t, p));
-            const bf16x4_t hi =
-                __builtin_amdgcn_ds_read_tr16_b64_v4bf16(EF_LDS(bf16x4_t, p + 16 * G::ROWB));
-            vx = bf16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            const u32x4_t c = __builtin_bit_cast(u32x4_t, f);
+            f = widen(c[0], c[1]);
           }
+          const int d = n % (DT / BATCH) * BATCH + i;
 #pragma unroll
           for (int r = 0; r < RT; ++r) {
             const u32x4_t pw = {pk[r][y][0], pk[r][y][1], pk[r][y][2], pk[r][y][3]};
-            oacc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                vx, __builtin_bit_cast(bf16x8_t, pw), oacc[r][i], 0, 0, 0);
+            oacc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                f, __builtin_bit_cast(bf16x8_t, pw), oacc[r][d], 0, 0, 0);
           }
         }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     };
     constexpr std::integral_constant<int, 0> s0{};
     constexpr std::integral_constant<int, 1> s1{};
     // (A stage is loaded again only when its reads have returned.)
     auto reads_done = [] { __builtin_amdgcn_s_waitcnt(0xc07f /* lgkmcnt(0) */); };
     if (j0 < j1) load(s0, j0);
-    for (int j = j0; j < j1; j += 2) {
-      if (j + 1 < j1) load(s1, j + 1);
-      compute(s0, j);
-      reads_done();
-      if (j + 2 < j1) load(s0, j + 2);
-      if (j + 1 < j1) compute(s1, j + 1);
-      reads_done();
-    }
-
-    // The waves' states meet in LDS, each lane's values at its own place.
+    // A query that is not finite: zero here, its row NaN where it sees a key.
+    bool poison[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      float l = lsum[t];
-      l += shfl_xor(l, 16);
-      l += shfl_xor(l, 32);
+      unsigned most = 0;
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) {
+        const u32x4_t v = __builtin_bit_cast(u32x4_t, qf[t][x]) ^ a.qflip;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          most = max(most, v[e] & 0x7fffu);
+          most = max(most, v[e] >> 16 & 0x7fffu);
+        }
+        qf[t][x] = __builtin_bit_cast(bf16x8_t, v);
+      }
+      // (bit patterns of bf16 magnitudes order as floats)
+      float y, z;
+      lane_pair<16>(__uint_as_float(most), y, z);
+      most = max(__float_as_uint(y), __float_as_uint(z));
+      lane_pair<32>(__uint_as_float(most), y, z);
+      most = max(__float_as_uint(y), __float_as_uint(z));
+      const bool bad = most >= 0x7f80u;
+      poison[t] = bad && lim[t] >= 0;
+      const bool drop = bad || 16 * t + l16 >= nrows;
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) {
+        u32x4_t v = __builtin_bit_cast(u32x4_t, qf[t][x]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = drop ? 0u : v[e];
+        qf[t][x] = __builtin_bit_cast(bf16x8_t, v);
+      }
+    }
+    for (int j = j0; j < j1; j += 2) {
+      load(s1, j + 1);
+      compute(s0, j);
+      reads_done();
+      load(s0, j + 2);
+      compute(s1, j + 1);
+      reads_done();
+    }
+    wait_loads<0>();
+
+    // The waves' states meet in LDS: values in a wave's own stages, each lane's at its place.
+    static_assert(ROWS * D * 4 <= 2 * kStageBytes && RT * DT * 1024 == ROWS * D * 4, "they fit");
+    constexpr int HALF = kStageBytes / 1024;  // fragments of a stage
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      float y, z;
+      lane_pair<16>(lsum[t], y, z);
+      float l = y + z;
+      lane_pair<32>(l, y, z);
+      l = y + z;
       if (poison[t] || lim[t] >= bad_from) l = __builtin_nanf("");
       if (g == 0) {
         sm[wave][16 * t + l16] = mref[t];
         sl[wave][16 * t + l16] = l;
       }
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        const int f = t * DT + i;
+        reinterpret_cast<floatx4*>(f < HALF ? sv0[wave] : sv1[wave])[f % HALF * 64 + lane] =
+            oacc[t][i];
+      }
     }
-    __syncthreads();  // (all reads of values are done too)
-    floatx4* const so = reinterpret_cast<floatx4*>(wave < 2 ? sv0 : sv1) + (wave & 1) * (ROWS * D / 4);
-    static_assert(2 * ROWS * D * 4 <= 4 * kStageBytes, "two waves' values in a stage");
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int i = 0; i < DT; ++i) so[(t * DT + i) * 64 + lane] = oacc[t][i];
     __syncthreads();
     const bool whole = u == first && u_next == first + units;
     const size_t slot = ((size_t)head * a.W + w) * 2 + (u == first ? 1 : 0);
+    const __amdgpu_buffer_rsrc_t acc_rs =
+        __builtin_amdgcn_make_buffer_rsrc(a.ws_acc, (short)0, -1, 0x00020000);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       const int r = 16 * t + l16;
@@ -464,8 +615,9 @@ void attn_paged_kernel(PagedParams a) {
         floatx4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const floatx4 z = reinterpret_cast<const floatx4*>(x < 2 ? sv0 : sv1)[(
-              (x & 1) * (ROWS * D / 4)) + (t * DT + i) * 64 + lane];
+          const int f = t * DT + i;
+          const floatx4 z = reinterpret_cast<const floatx4*>(
+              f < HALF ? sv0[x] : sv1[x])[f % HALF * 64 + lane];
 #pragma unroll
           for (int e = 0; e < 4; ++e) y[e] = fmaf(wt[x], z[e], y[e]);
         }
@@ -474,87 +626,100 @@ void attn_paged_kernel(PagedParams a) {
           const u32x2_t p = {pack_bf16x2(y[0] * inv, y[1] * inv),
                              pack_bf16x2(y[2] * inv, y[3] * inv)};
           *reinterpret_cast<u32x2_t*>(a.o + orow[t] + 16 * i + 4 * g) = p;
+        } else if (RT == 1 && a.counters != nullptr) {  // read by another workgroup of the launch
+          __builtin_amdgcn_raw_buffer_store_b128(
+              __builtin_bit_cast(u32x4_t, y), acc_rs,
+              (int)(((unsigned)(slot * ROWS + r) * D + 16 * i + 4 * g) * 4), 0,
+              16 /* device scope */);
         } else {
           *reinterpret_cast<floatx4*>(a.ws_acc + (slot * ROWS + r) * D + 16 * i + 4 * g) = y;
         }
       }
       if (!whole && valid && wave == 0 && g == 0) {
-        a.ws_m[slot * ROWS + r] = M;
-        a.ws_l[slot * ROWS + r] = L;
+        store_dev(a.ws_m + slot * ROWS + r, M);
+        store_dev(a.ws_l + slot * ROWS + r, L);
       }
     }
-    // The sequence's first part says where the others are.
-    if (u == first && threadIdx.x == 0) {
-      const int last = (first + units - 1) / T;
-      a.parts[(size_t)b * a.heads + head] = make_int2(w, last - w + 1);
+    const int w0 = (unsigned)first / (unsigned)T;
+    const int P = (unsigned)(first + units - 1) / (unsigned)T - w0 + 1;
+    if (RT == 2 || a.counters == nullptr) {
+      // The sequence's first part says where the others are.
+      if (u == first && threadIdx.x == 0) a.parts[(size_t)b * a.heads + head] = make_int2(w0, P);
+    } else if constexpr (RT == 1) if (!whole) {
+      // The last part to arrive joins them, a wave a row.
+      unsigned* const counter = a.counters + ((size_t)head * a.W + w0) * a.counter_stride;
+      const unsigned ticket = arrival_ticket(counter);
+      if (ticket >= (unsigned)(P - 1)) {
+        for (int r = wave; r < nrows; r += 4) {
+          const size_t slot0 = ((size_t)head * a.W + w0) * 2;
+          Joined j = {{0.f, 0.f, 0.f, 0.f}, 0.f, 0.f};
+          if (ticket == (unsigned)(P - 1))
+            j = join_parts<D, 8, true>(a, 0, P, [&](int p) {
+              return (slot0 + 2 * p + (p == 0 ? 1 : 0)) * ROWS + r;
+            });
+          // (A counter that was not zero: NaN.)
+          const float inv = ticket > (unsigned)(P - 1) ? __builtin_nanf("")
+                            : j.L == 0.f               ? 0.f
+                                                       : 1.f / j.L;
+          const int rr = row0 + r;
+          store_joined<D>(j, inv, a.o + ((size_t)(start + rr / a.G) * a.Hq +
+                                         (size_t)hk * a.G + rr % a.G) * D);
+        }
+        if (ticket == (unsigned)(P - 1) && threadIdx.x == 0) reset_counter(counter);
+      }
     }
-    u = u_next;
+    u = min(u_end, behind);
     __syncthreads();  // the stages may be loaded again
   }
 }
 
-// Joins the parts of a row that several workgroups share: one wave a row, D / 4 lanes a state.
+template <int D, bool E4M3, int RT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+void attn_paged_kernel(PagedParams a) {
+  attend_pages<D, E4M3, RT>(a);
+}
+
+// Joins the parts of a row that several workgroups share: four waves a row, each a quarter of
+// the parts.
 template <int D, int ROWS>
-__global__ __launch_bounds__(256) void paged_combine_kernel(PagedParams a) {
-  constexpr int LPS = D / 4, SPL = 64 / LPS, BATCH = 8;
+__global__ __launch_bounds__(256) void paged_combine_kernel(PagedParams a, int rows) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  constexpr int WGS = ROWS / 4;  // workgroups of a sequence's row tile
-  const int r = (int)(blockIdx.x % WGS) * 4 + wave;
-  const int head = (int)(blockIdx.x / WGS % a.heads);
-  const int b = (int)(blockIdx.x / WGS / a.heads);
+  const int r = (int)(blockIdx.x % rows);
+  const int head = (int)(blockIdx.x / rows % a.heads);
+  const int b = (int)(blockIdx.x / rows / a.heads);
   const int mt = head % a.mtiles, hk = head / a.mtiles;
   const int start = sequence_start(a.starts, b, a.B, a.T);
   const int n = min(max(sequence_start(a.starts, b + 1, a.B, a.T) - start, 0), a.T);
   const int row = mt * ROWS + r;
   if (row >= min(n, a.max_queries) * a.G) return;
   const int2 part = a.parts[(size_t)b * a.heads + head];
-  const int w0 = part.x, P = part.y;
+  const int P = part.y;
   if (P < 2) return;
-  auto state = [&](int p) {  // row of part p
-    return ((((size_t)head * a.W + w0 + p) * 2 + (p == 0 ? 1 : 0)) * ROWS + r);
-  };
-  const int grp = lane / LPS, ch = lane % LPS;
-  float M = kNegInf, L = 0.f;
-  floatx4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int p0 = 0; p0 < P; p0 += 64) {
-    const int count = min(P - p0, 64);
-    const bool have = lane < count;
-    const float m = have ? a.ws_m[state(p0 + lane)] : kNegInf;
-    const float l = have ? a.ws_l[state(p0 + lane)] : 0.f;
-    const float top = fmaxf(M, wave_max(m));
-    const float ref = top == kNegInf ? 0.f : top;
-    const float wt = exp2_fast(m - ref);  // base-2 units
-    const float old = exp2_fast(M - ref);
-    L = L * old + wave_sum(wt * l);
-    M = top;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] *= old;
-    for (int j = 0; j < count; j += BATCH * SPL) {
-      floatx4 y[BATCH];
-#pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        const int q = min(j + i * SPL + grp, count - 1);
-        y[i] = *reinterpret_cast<const floatx4*>(a.ws_acc + state(p0 + q) * D + 4 * ch);
-      }
-#pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        const int q = j + i * SPL + grp;
-        const float wq = __shfl(wt, min(q, 63), 64);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = q < count ? fmaf(wq, y[i][e], x[e]) : x[e];
-      }
-    }
+  const size_t slot0 = ((size_t)head * a.W + part.x) * 2;
+  __shared__ float sx[4][D], sm[4], sl[4];
+  Joined j = join_parts<D, 8, false>(a, P * wave / 4, P * (wave + 1) / 4, [&](int p) {
+    return (slot0 + 2 * p + (p == 0 ? 1 : 0)) * ROWS + r;
+  });
+  if (lane < D / 4) *reinterpret_cast<floatx4*>(&sx[wave][4 * lane]) = j.x;
+  if (lane == 0) {
+    sm[wave] = j.M;
+    sl[wave] = j.L;
   }
+  __syncthreads();
+  if (wave != 0) return;
+  const float M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  const float ref = M == kNegInf ? 0.f : M;
+  j = {{0.f, 0.f, 0.f, 0.f}, M, 0.f};
 #pragma unroll
-  for (int off = LPS; off < 64; off *= 2)
+  for (int x = 0; x < 4; ++x) {
+    const float wt = exp2_fast(sm[x] - ref);
+    j.L = fmaf(wt, sl[x], j.L);
+    if (lane < D / 4)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] += shfl_xor(x[e], off);
-  if (grp != 0) return;
-  const float inv = L == 0.f ? 0.f : 1.f / L;
-  const size_t orow =
-      ((size_t)(start + row / a.G) * a.Hq + (size_t)hk * a.G + row % a.G) * D;
-  const u32x2_t o = {pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv)};
-  *reinterpret_cast<u32x2_t*>(a.o + orow + 4 * ch) = o;
+      for (int e = 0; e < 4; ++e) j.x[e] = fmaf(wt, sx[x][4 * lane + e], j.x[e]);
+  }
+  store_joined<D>(j, j.L == 0.f ? 0.f : 1.f / j.L,
+                  a.o + ((size_t)(start + row / a.G) * a.Hq + (size_t)hk * a.G + row % a.G) * D);
 }
 
 template <int D, bool E4M3, int RT>
@@ -563,8 +728,9 @@ hipError_t launch(const PagedParams& a, hipStream_t stream) {
                      stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.counters != nullptr) return e;
-  const dim3 grid((unsigned)a.B * a.heads * (16 * RT / 4));
-  hipLaunchKernelGGL((paged_combine_kernel<D, 16 * RT>), grid, dim3(256), 0, stream, a);
+  const int rows = a.mtiles > 1 ? 16 * RT : a.rows;
+  const dim3 grid((unsigned)a.B * a.heads * rows);
+  hipLaunchKernelGGL((paged_combine_kernel<D, 16 * RT>), grid, dim3(256), 0, stream, a, rows);
   return hipGetLastError();
 }
 

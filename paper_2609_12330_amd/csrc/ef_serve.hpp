@@ -57,9 +57,11 @@ struct PagedParams {
   float* ws_l;
   float* ws_acc;       // [heads * W][2][rows][D]
   int T, B, Hq, Hkv, D, G;
+  int even;  // rows of a sequence without starts
   int max_queries;
   int rt;       // row tiles of 16 of a workgroup: 1 or 2
   int mtiles;   // workgroup tiles of a kv head's rows
+  int rows;     // most rows of a kv head: G max_queries
   int heads;    // Hkv * mtiles: what a launch deals out apart from each other
   int W;        // workgroups of each
   int counter_stride;
@@ -114,14 +116,15 @@ __device__ __forceinline__ int find_sequence(const int* starts, int B, int T, in
   return n - 1;
 }
 
-// Exclusive-to-inclusive sums over the wave's lanes.
+// Inclusive sums over the wave's lanes: within rows of 16, then rows 0 and 2 into the next ones,
+// then the first half into the second.
 __device__ __forceinline__ int wave_scan(int x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int off = 1; off < 64; off *= 2) {
-    const int y = __shfl_up(x, off, 64);
-    if (lane >= off) x += y;
-  }
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111 /* row_shr:1 */, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142 /* row_bcast:15 */, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143 /* row_bcast:31 */, 0xc, 0xf, false);
   return x;
 }
 #endif

@@ -82,17 +82,22 @@ constexpr int kFillWgs = 512;
 // Launch shape of attention over pages: see PagedParams. W workgroups share the keys of each
 // (kv head, row tile): the chip's 512 places, or one to a sequence where that is more.
 struct PagedPlan {
-  int rt, mtiles, heads, W;
+  int rt, mtiles, heads, W, rows;
+  bool fused;
   size_t parts_off, m_off, l_off, acc_off, bytes;
 };
 
 constexpr int kMostWgs = 2048;
+static_assert(kMostWgs * 64 <= ef::kCounterRegionBytes, "a counter for every workgroup");
+constexpr int kJoinElems = 1024;
+constexpr int kJoinParts = 128;
 
 ef_status paged_plan(PagedPlan& p, int T, int B, int Hq, int Hkv, int D, int max_queries) {
   const ef_status st = check_heads(T, B, Hq, Hkv, D);
   if (st != EF_OK) return st;
   if (max_queries < 0) return EF_ERR_INVALID_SHAPE;
   const long long rows = (long long)std::min(max_queries, T) * (Hq / Hkv);
+  p.rows = (int)rows;
   p.rt = rows <= 16 ? 1 : 2;
   const long long tile = 16 * p.rt, mtiles = (rows + tile - 1) / tile;
   if (mtiles * Hkv > kMaxGroups) return EF_ERR_INVALID_SHAPE;
@@ -101,7 +106,10 @@ ef_status paged_plan(PagedPlan& p, int T, int B, int Hq, int Hkv, int D, int max
   if (p.heads == 0) return EF_OK;
   p.W = std::max(1, std::max(kFillWgs / p.heads, std::min(B, kMostWgs / p.heads)));
   if ((long long)p.heads * p.W > kMaxGroups) return EF_ERR_INVALID_SHAPE;
-  if ((long long)B * p.heads * (tile / 4) > kMaxGroups) return EF_ERR_INVALID_SHAPE;
+  // The last of a row's parts joins them in the same launch where these are few (see below).
+  p.fused = rows * D <= kJoinElems && p.W <= kJoinParts && p.heads * p.W <= kMostWgs;
+  if (!p.fused && (long long)B * p.heads * std::min(rows, tile) > kMaxGroups)
+    return EF_ERR_INVALID_SHAPE;
   const size_t states = (size_t)p.heads * p.W * 2 * tile;
   p.parts_off = ef::kCounterRegionBytes;
   p.m_off = p.parts_off + ef::ws_align256((size_t)B * p.heads * sizeof(int2));
@@ -252,7 +260,8 @@ ef_status ef_attention_paged(const void* q, const void* k_cache, const void* v_c
   st = check_pages(pages, page, width, format);
   if (st != EF_OK) return st;
   // The units of work of a head are counted in 32 bits.
-  if ((long long)B * ((long long)width * page / 64 + 1) >= (1LL << 31)) return EF_ERR_INVALID_SHAPE;
+  if ((long long)B * ((long long)width * page / 64 + 32) >= (1LL << 31))
+    return EF_ERR_INVALID_SHAPE;
   if (!std::isfinite(scale)) return EF_ERR_INVALID_SCALE;
   if (T == 0 || B == 0) return EF_OK;
   if (uneven(starts, T, B) || (starts == nullptr && max_queries < T / B))
@@ -272,14 +281,19 @@ ef_status ef_attention_paged(const void* q, const void* k_cache, const void* v_c
   a.lengths = lengths;
   a.starts = starts;
   a.parts = reinterpret_cast<int2*>(ws + p.parts_off);
+  a.counters = p.fused ? reinterpret_cast<unsigned*>(ws) : nullptr;
+  // Counters lie as far apart as there is room for.
+  a.counter_stride = p.heads * p.W <= ef::kCounterSlots ? ef::kCounterStride : 16;
   a.ws_m = reinterpret_cast<float*>(ws + p.m_off);
   a.ws_l = reinterpret_cast<float*>(ws + p.l_off);
   a.ws_acc = reinterpret_cast<float*>(ws + p.acc_off);
   a.T = T; a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.D = D;
   a.G = Hq / Hkv;
+  a.even = T / B;
   a.max_queries = max_queries;
   a.rt = p.rt;
   a.mtiles = p.mtiles;
+  a.rows = p.rows;
   a.heads = p.heads;
   a.W = p.W;
   // The floor keeps a zero scale well defined (every visible key gets weight 1).
