@@ -31,7 +31,7 @@ namespace {
 constexpr int kUnit = 64;             // keys of a unit of work
 // Bytes of keys that a sequence counts beside its own: what a workgroup takes from one sequence to the
 // next (rows, table, the first loads' way, the join of its waves).
-constexpr int kExtraBytes = 128 * 1024;
+constexpr int kExtraBytes = 64 * 1024;
 constexpr float kHeadroom = 8.f;      // base-2 headroom before the reference moves
 constexpr int kStageBytes = 8192;     // keys, and values, of a wave's step
 // A value that is the same in all lanes, for the compiler to see.
@@ -233,6 +233,29 @@ __device__ __forceinline__ void attend_pages(const PagedParams& a) {
     const int u_next = min(u_end, first + units);
     const int k1 = min((u_next - first) * kUnit, end_seen);
 
+    // This wave's steps.
+    const int steps = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0;
+    const int j0 = uniform(steps * wave / 4), j1 = uniform(steps * (wave + 1) / 4);
+    int wend = uniform(min(k1, k0 + j1 * KT));  // keys it may read
+    int bad_from = 0x7fffffff;                  // first key of a page that is none
+    const int page_mask = (1 << a.c.shift) - 1;
+    // Table entries p0 .. p0 + 63, one to a lane (from the last one on, that one).
+    const int* const table = a.c.table + (size_t)b * a.c.width;
+    int p0 = uniform((k0 + j0 * KT) >> a.c.shift), pv = 0;
+    auto entries = [&] { return table[min(p0 + lane, max((wend - 1) >> a.c.shift, 0))]; };
+    auto check_entries = [&] {
+      const bool bad = (unsigned)pv >= (unsigned)a.c.pages;
+      const auto none = __builtin_amdgcn_ballot_w64(bad);
+      if (none) {  // the walk ends in front of it
+        const int from = (p0 + __builtin_ctzll(none)) << a.c.shift;
+        if (from < wend) bad_from = from;
+        wend = uniform(min(wend, from));
+        pv = bad ? 0 : pv;
+      }
+    };
+    const bool some = k1 > k0;  // (else the rows see no key at all)
+    if (some) pv = entries();
+
     // Rows: queries, the last key they see.
     bf16x8_t qf[RT][D / 32];
     int lim[RT];
@@ -268,15 +291,6 @@ __device__ __forceinline__ void attend_pages(const PagedParams& a) {
       for (int i = 0; i < DT; ++i) oacc[t][i] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // This wave's steps.
-    const int steps = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0;
-    const int j0 = uniform(steps * wave / 4), j1 = uniform(steps * (wave + 1) / 4);
-    int wend = uniform(min(k1, k0 + j1 * KT));  // keys it may read
-    int bad_from = 0x7fffffff;         // first key of a page that is none
-    int pv = 0, p0 = -0x10000000;      // table entries p0 .. p0 + 63, one to a lane
-    const int* const table = a.c.table + (size_t)b * a.c.width;
-    const int page_mask = (1 << a.c.shift) - 1;
-
     u32x4_t kx[2][8];
     // First row of 16 keys (which lie in one page) in the cache of this head.
     auto cell_of = [&](int key) -> size_t {
@@ -288,16 +302,8 @@ __device__ __forceinline__ void attend_pages(const PagedParams& a) {
       const int kb = k0 + j * KT;
       if (((min(kb + KT, wend) - 1) >> a.c.shift) - p0 >= 64) {
         p0 = uniform(kb >> a.c.shift);
-        const int last = (wend - 1) >> a.c.shift;
-        const bool used = p0 + lane <= last;
-        pv = used ? table[p0 + lane] : 0;
-        const bool bad = (unsigned)pv >= (unsigned)a.c.pages;
-        const auto none = __builtin_amdgcn_ballot_w64(bad);
-        if (none) {  // the walk ends in front of it
-          bad_from = (p0 + __builtin_ctzll(none)) << a.c.shift;
-          wend = uniform(min(wend, bad_from));
-          pv = bad ? 0 : pv;
-        }
+        pv = entries();
+        check_entries();
       }
       // Each 16 keys have a buffer of their own that ends behind the last one the wave may read:
       // rows past it are zeros (masked later), and a step past it as a whole moves nothing, but
@@ -524,7 +530,8 @@ __device__ __forceinline__ void attend_pages(const PagedParams& a) {
     constexpr std::integral_constant<int, 1> s1{};
     // (A stage is loaded again only when its reads have returned.)
     auto reads_done = [] { __builtin_amdgcn_s_waitcnt(0xc07f /* lgkmcnt(0) */); };
-    if (j0 < j1) load(s0, j0);
+    check_entries();
+    load(s0, j0);
     // A query that is not finite: zero here, its row NaN where it sees a key.
     bool poison[RT];
 #pragma unroll
@@ -679,44 +686,47 @@ void attn_paged_kernel(PagedParams a) {
   attend_pages<D, E4M3, RT>(a);
 }
 
-// Joins the parts of a row that several workgroups share: four waves a row, each a quarter of
-// the parts.
-template <int D, int ROWS>
-__global__ __launch_bounds__(256) void paged_combine_kernel(PagedParams a, int rows) {
+// Joins the parts of a row that several workgroups share: WPR waves a row, each its share of the
+// parts.
+template <int D, int ROWS, int WPR>
+__global__ __launch_bounds__(256) void paged_combine_kernel(PagedParams a, int tiles) {
+  constexpr int RPW = 4 / WPR;  // rows of a workgroup
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r = (int)(blockIdx.x % rows);
-  const int head = (int)(blockIdx.x / rows % a.heads);
-  const int b = (int)(blockIdx.x / rows / a.heads);
+  const int r = (int)(blockIdx.x % tiles) * RPW + wave / WPR;
+  const int head = (int)(blockIdx.x / tiles % a.heads);
+  const int b = (int)(blockIdx.x / tiles / a.heads);
   const int mt = head % a.mtiles, hk = head / a.mtiles;
+  const int2 part = a.parts[(size_t)b * a.heads + head];
   const int start = sequence_start(a.starts, b, a.B, a.T);
   const int n = min(max(sequence_start(a.starts, b + 1, a.B, a.T) - start, 0), a.T);
   const int row = mt * ROWS + r;
-  if (row >= min(n, a.max_queries) * a.G) return;
-  const int2 part = a.parts[(size_t)b * a.heads + head];
-  const int P = part.y;
-  if (P < 2) return;
+  // (Without rows in this tile nothing wrote `part`. All waves of a row end here, or none.)
+  if (r >= ROWS || row >= min(n, a.max_queries) * a.G || part.y < 2) return;
+  const int P = part.y, x = wave % WPR;
   const size_t slot0 = ((size_t)head * a.W + part.x) * 2;
-  __shared__ float sx[4][D], sm[4], sl[4];
-  Joined j = join_parts<D, 8, false>(a, P * wave / 4, P * (wave + 1) / 4, [&](int p) {
+  Joined j = join_parts<D, 8, false>(a, P * x / WPR, P * (x + 1) / WPR, [&](int p) {
     return (slot0 + 2 * p + (p == 0 ? 1 : 0)) * ROWS + r;
   });
-  if (lane < D / 4) *reinterpret_cast<floatx4*>(&sx[wave][4 * lane]) = j.x;
-  if (lane == 0) {
-    sm[wave] = j.M;
-    sl[wave] = j.L;
-  }
-  __syncthreads();
-  if (wave != 0) return;
-  const float M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-  const float ref = M == kNegInf ? 0.f : M;
-  j = {{0.f, 0.f, 0.f, 0.f}, M, 0.f};
+  if constexpr (WPR > 1) {
+    __shared__ float sx[4][D], sm[4], sl[4];
+    if (lane < D / 4) *reinterpret_cast<floatx4*>(&sx[wave][4 * lane]) = j.x;
+    if (lane == 0) {
+      sm[wave] = j.M;
+      sl[wave] = j.L;
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    const float M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+    const float ref = M == kNegInf ? 0.f : M;
+    j = {{0.f, 0.f, 0.f, 0.f}, M, 0.f};
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    const float wt = exp2_fast(sm[x] - ref);
-    j.L = fmaf(wt, sl[x], j.L);
-    if (lane < D / 4)
+    for (int y = 0; y < 4; ++y) {
+      const float wt = exp2_fast(sm[y] - ref);
+      j.L = fmaf(wt, sl[y], j.L);
+      if (lane < D / 4)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) j.x[e] = fmaf(wt, sx[x][4 * lane + e], j.x[e]);
+        for (int e = 0; e < 4; ++e) j.x[e] = fmaf(wt, sx[y][4 * lane + e], j.x[e]);
+    }
   }
   store_joined<D>(j, j.L == 0.f ? 0.f : 1.f / j.L,
                   a.o + ((size_t)(start + row / a.G) * a.Hq + (size_t)hk * a.G + row % a.G) * D);
@@ -728,9 +738,15 @@ hipError_t launch(const PagedParams& a, hipStream_t stream) {
                      stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.counters != nullptr) return e;
+  // A wave a row where the parts may be few, four where there may be hundreds.
   const int rows = a.mtiles > 1 ? 16 * RT : a.rows;
-  const dim3 grid((unsigned)a.B * a.heads * rows);
-  hipLaunchKernelGGL((paged_combine_kernel<D, 16 * RT>), grid, dim3(256), 0, stream, a, rows);
+  const bool wide = a.W > 128;
+  const int tiles = wide ? rows : (rows + 3) / 4;
+  const dim3 grid((unsigned)a.B * a.heads * tiles);
+  if (wide)
+    hipLaunchKernelGGL((paged_combine_kernel<D, 16 * RT, 4>), grid, dim3(256), 0, stream, a, tiles);
+  else
+    hipLaunchKernelGGL((paged_combine_kernel<D, 16 * RT, 1>), grid, dim3(256), 0, stream, a, tiles);
   return hipGetLastError();
 }
 
