@@ -88,7 +88,7 @@ SIGNATURES = {
     "ef_attention_shared_prefix": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i,
                                         _i, _f, _i, _vp, _sz, _vp]),
     "ef_attention_shared_prefix_workspace_size": (_sz, [_i, _i, _i, _i, _i, _i, _i]),
-    "ef_rope": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _d, _i, _vp]),
+    "ef_rope": (_i, [_vp] * 4 + [_i] * 5 + [_d, _i, _vp]),
     "ef_cache_write": (_i, [_vp] * 12 + [_i] * 11 + [_d, _vp]),
     "ef_cache_read": (_i, [_vp] * 8 + [_i] * 8 + [_vp]),
     "ef_attention_paged": (_i, [_vp] * 9 + [_i] * 10 + [_f, _vp, _sz, _vp]),
@@ -744,10 +744,18 @@ def _current_device():
 def _call_on(t, stream, fn, *args):
     """fn(*args, stream handle) with t's device current: a launch needs the device of its
     stream, and the current stream of another device is not the one t's work is ordered on."""
-    if stream is not None and stream.device != t.device:
+    if stream is None:
+        dev = t.get_device()
+        if _current_device() == dev:
+            try:
+                handle = _TORCH._C._cuda_getCurrentRawStream(dev)
+            except AttributeError:
+                handle = _stream_handle(None)
+            return fn(*args, handle)
+    elif stream.device != t.device:
         raise ValueError(f"stream is on {stream.device}, the tensors are on {t.device}")
-    if _current_device() == t.get_device():
-        return fn(*args, _stream_handle(stream))
+    elif _current_device() == t.get_device():
+        return fn(*args, stream.cuda_stream)
     with _torch().cuda.device(t.device):
         return fn(*args, _stream_handle(stream))
 
@@ -990,46 +998,68 @@ def make_rope(rot: int, base: float = 10000.0, interleaved: bool = False, scalin
     return Rope(t.to(device), interleaved, amplitude)
 
 
+# As above, the conditions are tested together, and a call that breaks one goes through them by
+# name.
+
+
 def _ints(t, name, n, ref):
     _check_tensor(t, name, _torch().int32, 1, ref)
     if t.shape[0] != n:
         raise ValueError(f"{name} must have {n} entries, got {t.shape[0]}")
-    return t.data_ptr()
 
 
-def _rows3(t, name, ref=None):
+def _rows3(t, name, ref=None, shape=None):
     _check_tensor(t, name, _torch().bfloat16, 3, ref)
-    return t.shape
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
 
 
-def _out3(x, out, stream, name="out"):
-    if out is None:
-        return _new(x.shape, _torch().bfloat16, x, stream)
-    _check_tensor(out, name, _torch().bfloat16, 3, x)
-    if out.shape != x.shape:
-        raise ValueError(f"{name} must be {tuple(x.shape)}, got {tuple(out.shape)}")
-    return out
+def _table_and_lengths(table, lengths, starts, T, ref):
+    """Raises the error of the first that does not fit the T rows of B sequences."""
+    _check_tensor(table, "table", _torch().int32, 2, ref)
+    B = table.shape[0]
+    _ints(lengths, "lengths", B, ref)
+    if starts is not None:
+        _ints(starts, "starts", B + 1, ref)
+    elif B and T % B:
+        raise ValueError(f"without starts every sequence has as many rows: {T} are not {B} times "
+                         "a number")
 
 
-def _rope_args(rope, ref):
-    if rope is None:
-        return None, 0, False, 1.0
-    if rope.turns.get_device() != ref.get_device():
-        _same_device(rope.turns, ref, "rope")
-    return rope.turns.data_ptr(), rope.rot, rope.interleaved, rope.amplitude
+def _same_cache(cache, ref, D, H=None):
+    if cache.k.get_device() != ref.get_device():
+        _same_device(cache.k, ref, "cache")
+    Hc, Dc = cache.shape[1], cache.shape[3]
+    if Dc != D or (H is not None and Hc != H):
+        raise ValueError(f"the cache holds rows [{Hc}, {Dc}], the tensors have [{H}, {D}]")
 
 
 def rope(x, positions, rope: Rope, transpose: bool = False, out=None, stream=None):
     """Rows x [T, H, D] turned to their positions (int32 [T], on the GPU) through ef_rope; with
     transpose the transposed map, which takes the gradient of the result to that of x. `out` may
     be x."""
-    T, H, D = _rows3(x, "x")
-    p = _ints(positions, "positions", T, x)
-    turns, rot, interleaved, amplitude = _rope_args(rope, x)
-    o = _out3(x, out, stream)
-    st = _call_on(x, stream, ef_rope, x.data_ptr(), p, turns, o.data_ptr(), T, H, D, rot,
-                  interleaved, amplitude, transpose)
-    _check(st, "ef_rope")
+    torch = _torch()
+    bf16 = torch.bfloat16
+    turns = rope.turns
+    o = x if out is None else out
+    dev = x.get_device()
+    if not (x.dtype is bf16 and o.dtype is bf16 and positions.dtype is torch.int32 and
+            x.is_contiguous() and o.is_contiguous() and positions.is_contiguous() and
+            x.dim() == 3 and positions.dim() == 1 and dev >= 0 and o.get_device() == dev and
+            positions.get_device() == dev and turns.get_device() == dev and
+            (out is None or o.shape == x.shape) and positions.shape[0] == x.shape[0]):
+        _rows3(x, "x")
+        _ints(positions, "positions", x.shape[0], x)
+        _same_device(turns, x, "rope")
+        _rows3(o, "out", x, x.shape)
+    if out is None:
+        o = _new(x.shape, bf16, x, stream)
+    T, H, D = x.shape
+    st = _call_on(x, stream, _lib().ef_rope, x.data_ptr(), positions.data_ptr(), turns.data_ptr(),
+                  o.data_ptr(), T, H, D, rope.rot, rope.interleaved, rope.amplitude,
+                  1 if transpose else 0)
+    if st:
+        _check(st, "ef_rope")
     return o
 
 
@@ -1037,7 +1067,7 @@ class PagedCache:
     """A key-value cache in pages: k and v [pages, Hkv, page, D], bfloat16, or float8_e4m3fn with
     float32 scales [pages, Hkv, page] for every row of either."""
 
-    __slots__ = ("k", "v", "k_scale", "v_scale", "format", "_args")
+    __slots__ = ("k", "v", "k_scale", "v_scale", "format", "shape")
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         torch = _torch()
@@ -1056,13 +1086,13 @@ class PagedCache:
                     raise ValueError(f"{name} must be {tuple(k.shape[:3])}, got {tuple(t.shape)}")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.format = CACHE_E4M3 if e4m3 else CACHE_BF16
-        self._args = (k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if e4m3 else None,
-                      v_scale.data_ptr() if e4m3 else None)
+        self.shape = tuple(k.shape)  # (pages, Hkv, page, D)
 
-    @property
-    def shape(self):
-        """(pages, Hkv, page, D)"""
-        return self.k.shape
+    def _args(self):
+        if self.k_scale is None:
+            return self.k.data_ptr(), self.v.data_ptr(), None, None
+        return (self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
+                self.v_scale.data_ptr())
 
 
 def make_cache(pages: int, Hkv: int, page: int, D: int, e4m3: bool = False, device="cuda"):
@@ -1075,82 +1105,99 @@ def make_cache(pages: int, Hkv: int, page: int, D: int, e4m3: bool = False, devi
     return PagedCache(*kv)
 
 
-def _table(table, ref, B=None):
-    _check_tensor(table, "table", _torch().int32, 2, ref)
-    if B is not None and table.shape[0] != B:
-        raise ValueError(f"table must have {B} rows, got {table.shape[0]}")
-    return table.shape
-
-
-def _starts_ptr(starts, T, B, ref):
-    if starts is not None:
-        return _ints(starts, "starts", B + 1, ref)
-    if B and T % B:
-        raise ValueError(f"without starts every sequence has as many rows: {T} are not {B} times "
-                         "a number")
-    return None
-
-
 def cache_write(cache: PagedCache, k, v, table, lengths, starts=None, q=None,
                 rope: Optional[Rope] = None, q_out=None, stream=None):
     """Appends the new tokens k, v [T, Hkv, D] of B sequences to the cache through ef_cache_write,
     rotated by `rope`; returns q [T, Hq, D] rotated beside them (None without q; q_out may be q).
     table [B, width] int32 names the sequences' pages, lengths [B] int32 their keys, the new ones
     among them, and starts [B + 1] int32 their rows, T / B each without it."""
-    T, H, D = _rows3(k, "k")
-    if _rows3(v, "v", k) != k.shape:
-        raise ValueError("v must be shaped like k")
-    pages, Hc, page, Dc = cache.shape
-    if (Hc, Dc) != (H, D):
-        raise ValueError(f"the cache holds rows [{Hc}, {Dc}], k has [{H}, {D}]")
-    if cache.k.get_device() != k.get_device():
-        _same_device(cache.k, k, "cache")
-    B, width = _table(table, k)
-    n = _ints(lengths, "lengths", B, k)
-    s = _starts_ptr(starts, T, B, k)
-    turns, rot, interleaved, amplitude = _rope_args(rope, k)
+    torch = _torch()
+    bf16, i32 = torch.bfloat16, torch.int32
+    dev = k.get_device()
+    pages, H, page, D = cache.shape
+    if not (k.dtype is bf16 and v.dtype is bf16 and table.dtype is i32 and lengths.dtype is i32 and
+            k.is_contiguous() and v.is_contiguous() and table.is_contiguous() and
+            lengths.is_contiguous() and dev >= 0 and v.get_device() == dev and
+            table.get_device() == dev and lengths.get_device() == dev and
+            cache.k.get_device() == dev and k.dim() == 3 and k.shape == v.shape and
+            k.shape[1] == H and k.shape[2] == D and table.dim() == 2 and lengths.dim() == 1 and
+            lengths.shape[0] == table.shape[0] > 0 and
+            (k.shape[0] % table.shape[0] == 0 if starts is None else
+             starts.dtype is i32 and starts.is_contiguous() and starts.get_device() == dev and
+             starts.dim() == 1 and starts.shape[0] == table.shape[0] + 1)):
+        _rows3(k, "k")
+        _rows3(v, "v", k, k.shape)
+        _same_cache(cache, k, k.shape[2], k.shape[1])
+        _table_and_lengths(table, lengths, starts, k.shape[0], k)
+    T = k.shape[0]
+    B, width = table.shape
     Hq, qp, op = 0, None, None
     if q is not None:
-        Tq, Hq, Dq = _rows3(q, "q", k)
-        if (Tq, Dq) != (T, D):
-            raise ValueError(f"q must be [{T}, Hq, {D}], got {tuple(q.shape)}")
-        q_out = _out3(q, q_out, stream, "q_out")
-        qp, op = q.data_ptr(), q_out.data_ptr()
+        o = q if q_out is None else q_out
+        if not (q.dtype is bf16 and o.dtype is bf16 and q.is_contiguous() and o.is_contiguous() and
+                q.get_device() == dev and o.get_device() == dev and q.dim() == 3 and
+                (o is q or o.shape == q.shape) and q.shape[0] == T and q.shape[2] == D):
+            _rows3(q, "q", k)
+            _rows3(q, "q", k, (T, q.shape[1], D))
+            _rows3(o, "q_out", k, q.shape)
+        if q_out is None:
+            q_out = _new(q.shape, bf16, q, stream)
+        Hq, qp, op = q.shape[1], q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out needs q")
-    st = _call_on(k, stream, ef_cache_write, k.data_ptr(), v.data_ptr(), qp, turns, *cache._args,
-                  table.data_ptr(), n, s, op, T, B, Hq, H, D, pages, page, width, cache.format,
-                  rot, interleaved, amplitude)
-    _check(st, "ef_cache_write")
+    turns, rot, interleaved, amplitude = None, 0, False, 1.0
+    if rope is not None:
+        if rope.turns.get_device() != dev:
+            _same_device(rope.turns, k, "rope")
+        turns, rot = rope.turns.data_ptr(), rope.rot
+        interleaved, amplitude = rope.interleaved, rope.amplitude
+    st = _call_on(k, stream, _lib().ef_cache_write, k.data_ptr(), v.data_ptr(), qp, turns,
+                  *cache._args(), table.data_ptr(), lengths.data_ptr(),
+                  None if starts is None else starts.data_ptr(), op, T, B, Hq, H, D, pages, page,
+                  width, cache.format, rot, interleaved, amplitude)
+    if st:
+        _check(st, "ef_cache_write")
     return q_out
 
 
 def cache_read(cache: PagedCache, table, starts, total: Optional[int] = None, k_out=None,
                v_out=None, stream=None):
     """The first starts[b + 1] - starts[b] cached rows of every sequence as packed bf16 rows k, v
-    [total, Hkv, D], through ef_cache_read. `total` may be left out where k_out and v_out are given;
+    [total, Hkv, D], through ef_cache_read. `total` may be left out where k_out or v_out is given;
     rows that belong to no sequence are left as they were."""
-    B, width = _table(table, cache.k)
-    s = _ints(starts, "starts", B + 1, cache.k)
+    torch = _torch()
+    bf16, i32 = torch.bfloat16, torch.int32
     pages, H, page, D = cache.shape
+    dev = cache.k.get_device()
     if total is None:
-        if k_out is None or v_out is None:
-            raise ValueError("cache_read needs total, or k_out and v_out")
-        total = k_out.shape[0]
-    outs = []
-    for name, t in (("k_out", k_out), ("v_out", v_out)):
-        if t is None:
-            t = _new((total, H, D), _torch().bfloat16, cache.k, stream)
-        else:
-            _check_tensor(t, name, _torch().bfloat16, 3, cache.k)
-            if t.shape != (total, H, D):
-                raise ValueError(f"{name} must be [{total}, {H}, {D}], got {tuple(t.shape)}")
-        outs.append(t)
-    st = _call_on(cache.k, stream, ef_cache_read, *cache._args, table.data_ptr(), s,
-                  outs[0].data_ptr(), outs[1].data_ptr(), total, B, H, D, pages, page, width,
-                  cache.format)
-    _check(st, "ef_cache_read")
-    return tuple(outs)
+        if k_out is None and v_out is None:
+            raise ValueError("cache_read needs total, or k_out or v_out")
+        total = (v_out if k_out is None else k_out).shape[0]
+    if total < 0:
+        raise ValueError("total must not be negative")
+    shape = (total, H, D)
+    if k_out is None:
+        k_out = _new(shape, bf16, cache.k, stream)
+    if v_out is None:
+        v_out = _new(shape, bf16, cache.k, stream)
+    if not (table.dtype is i32 and starts.dtype is i32 and k_out.dtype is bf16 and
+            v_out.dtype is bf16 and table.is_contiguous() and starts.is_contiguous() and
+            k_out.is_contiguous() and v_out.is_contiguous() and table.get_device() == dev and
+            starts.get_device() == dev and k_out.get_device() == dev and
+            v_out.get_device() == dev and table.dim() == 2 and starts.dim() == 1 and
+            k_out.shape == shape and v_out.shape == shape and
+            starts.shape[0] == table.shape[0] + 1):
+        _check_tensor(table, "table", i32, 2, cache.k)
+        _ints(starts, "starts", table.shape[0] + 1, cache.k)
+        _rows3(k_out, "k_out", cache.k, shape)
+        _rows3(v_out, "v_out", cache.k, shape)
+    B, width = table.shape
+    st = _call_on(cache.k, stream, _lib().ef_cache_read, *cache._args(), table.data_ptr(),
+                  starts.data_ptr(), k_out.data_ptr(), v_out.data_ptr(), total, B, H, D, pages,
+                  page, width, cache.format)
+    if st:
+        _check(st, "ef_cache_read")
+    return k_out, v_out
 
 
 def make_paged_workspace(q, cache: PagedCache, B: int, max_queries: int = 1, stream=None):
@@ -1169,28 +1216,42 @@ def attention_paged(q, cache: PagedCache, table, lengths, starts=None,
     among them, through ef_attention_paged; token i of n sees the positions up to lengths[b] - n +
     i. starts [B + 1] int32 are the sequences' rows, T / B each without it; max_queries is the
     most rows of a sequence, needed with starts. Returns bf16 shaped like q."""
-    T, Hq, D = _rows3(q, "q")
+    torch = _torch()
+    bf16, i32 = torch.bfloat16, torch.int32
+    dev = q.get_device()
     pages, H, page, Dc = cache.shape
-    if Dc != D:
-        raise ValueError(f"the cache holds rows of {Dc}, q has {D}")
-    if cache.k.get_device() != q.get_device():
-        _same_device(cache.k, q, "cache")
-    B, width = _table(table, q)
-    n = _ints(lengths, "lengths", B, q)
-    s = _starts_ptr(starts, T, B, q)
+    o = q if out is None else out
+    if not (q.dtype is bf16 and o.dtype is bf16 and table.dtype is i32 and lengths.dtype is i32 and
+            q.is_contiguous() and o.is_contiguous() and table.is_contiguous() and
+            lengths.is_contiguous() and dev >= 0 and o.get_device() == dev and
+            table.get_device() == dev and lengths.get_device() == dev and
+            cache.k.get_device() == dev and q.dim() == 3 and q.shape[2] == Dc and
+            (o is q or o.shape == q.shape) and table.dim() == 2 and lengths.dim() == 1 and
+            lengths.shape[0] == table.shape[0] > 0 and
+            (q.shape[0] % table.shape[0] == 0 if starts is None else
+             starts.dtype is i32 and starts.is_contiguous() and starts.get_device() == dev and
+             starts.dim() == 1 and starts.shape[0] == table.shape[0] + 1)):
+        _rows3(q, "q")
+        _same_cache(cache, q, q.shape[2])
+        _table_and_lengths(table, lengths, starts, q.shape[0], q)
+        _rows3(o, "out", q, q.shape)
+    T, Hq, D = q.shape
+    B, width = table.shape
     if max_queries is None:
         if starts is not None:
             raise ValueError("starts need max_queries, the most rows of a sequence")
         max_queries = T // B if B else 0
-    if scale is None:
-        scale = 1.0 / math.sqrt(D)
-    o = _out3(q, out, stream)
+    if out is None:
+        o = _new(q.shape, bf16, q, stream)
     ptr, nbytes, workspace = _own_workspace(workspace, ef_attention_paged_workspace_size,
                                             (T, B, Hq, H, D, max_queries), q, stream)
-    st = _call_on(q, stream, ef_attention_paged, q.data_ptr(), *cache._args, table.data_ptr(), n, s,
-                  o.data_ptr(), T, B, Hq, H, D, max_queries, pages, page, width, cache.format,
-                  float(scale), ptr, nbytes)
-    _check(st, "ef_attention_paged")
+    st = _call_on(q, stream, _lib().ef_attention_paged, q.data_ptr(), *cache._args(),
+                  table.data_ptr(), lengths.data_ptr(),
+                  None if starts is None else starts.data_ptr(), o.data_ptr(), T, B, Hq, H, D,
+                  max_queries, pages, page, width, cache.format,
+                  1.0 / math.sqrt(D) if scale is None else float(scale), ptr, nbytes)
+    if st:
+        _check(st, "ef_attention_paged")
     return o
 
 
@@ -1208,22 +1269,39 @@ def attention_packed(q, k, v, starts, k_starts=None, causal: bool = True,
     1 of q [T, Hq, D] over rows k_starts[b] .. k_starts[b + 1] - 1 of k, v [Tk, Hkv, D] (starts,
     where k_starts is left out), the last ones of which are the rows' own with `causal`. Returns
     bf16 shaped like q."""
-    T, Hq, D = _rows3(q, "q")
-    Tk, H, Dk = _rows3(k, "k", q)
-    if _rows3(v, "v", q) != k.shape or Dk != D:
-        raise ValueError("k and v must be [Tk, Hkv, D] matching q")
-    _check_tensor(starts, "starts", _torch().int32, 1, q)
+    torch = _torch()
+    bf16, i32 = torch.bfloat16, torch.int32
+    dev = q.get_device()
+    ks = starts if k_starts is None else k_starts
+    o = q if out is None else out
+    if not (q.dtype is bf16 and k.dtype is bf16 and v.dtype is bf16 and o.dtype is bf16 and
+            starts.dtype is i32 and ks.dtype is i32 and q.is_contiguous() and
+            k.is_contiguous() and v.is_contiguous() and o.is_contiguous() and
+            starts.is_contiguous() and ks.is_contiguous() and dev >= 0 and
+            k.get_device() == dev and v.get_device() == dev and o.get_device() == dev and
+            starts.get_device() == dev and ks.get_device() == dev and q.dim() == 3 and
+            k.dim() == 3 and k.shape == v.shape and k.shape[2] == q.shape[2] and
+            (o is q or o.shape == q.shape) and starts.dim() == 1 and
+            (ks is starts or ks.shape == starts.shape) and starts.shape[0] > 0):
+        _rows3(q, "q")
+        _rows3(k, "k", q)
+        _rows3(k, "k", q, (k.shape[0], k.shape[1], q.shape[2]))
+        _rows3(v, "v", q, k.shape)
+        _check_tensor(starts, "starts", i32, 1, q)
+        if starts.shape[0] == 0:
+            raise ValueError("starts must have an entry more than there are sequences")
+        _ints(ks, "k_starts", starts.shape[0], q)
+        _rows3(o, "out", q, q.shape)
+    T, Hq, D = q.shape
+    Tk, H, _ = k.shape
     B = starts.shape[0] - 1
-    if B < 0:
-        raise ValueError("starts must have an entry more than there are sequences")
-    ks = starts.data_ptr() if k_starts is None else _ints(k_starts, "k_starts", B + 1, q)
-    if scale is None:
-        scale = 1.0 / math.sqrt(D)
-    o = _out3(q, out, stream)
+    if out is None:
+        o = _new(q.shape, bf16, q, stream)
     ptr, nbytes, workspace = _own_workspace(workspace, ef_attention_packed_workspace_size,
                                             (T, Tk, B, Hq, H, D), q, stream)
-    st = _call_on(q, stream, ef_attention_packed, q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                  starts.data_ptr(), ks, o.data_ptr(), T, Tk, B, Hq, H, D, float(scale), causal,
-                  ptr, nbytes)
-    _check(st, "ef_attention_packed")
+    st = _call_on(q, stream, _lib().ef_attention_packed, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                  starts.data_ptr(), ks.data_ptr(), o.data_ptr(), T, Tk, B, Hq, H, D,
+                  1.0 / math.sqrt(D) if scale is None else float(scale), 1 if causal else 0, ptr, nbytes)
+    if st:
+        _check(st, "ef_attention_packed")
     return o
