@@ -33,8 +33,9 @@ struct RowsParams {
   int rot, interleaved;
   double amplitude;
   int transpose;
-  int per;     // tokens of a workgroup, 1 .. 4
+  int per;     // tokens of a workgroup, 1 .. 16
   int blocks;  // workgroups that share the rows of these tokens
+  int once;    // stores are non-temporal
 };
 
 struct CacheReadParams {
@@ -43,6 +44,8 @@ struct CacheReadParams {
   uint16_t* k_out;    // [T][Hkv][D]
   uint16_t* v_out;
   int T, B, Hkv, D;
+  int per;   // tokens of a workgroup, 1 .. 16
+  int once;  // stores are non-temporal
 };
 
 struct PagedParams {

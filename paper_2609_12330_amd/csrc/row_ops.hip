@@ -3,7 +3,7 @@
 // A pair (a, b) of a row turns by the angle 2 pi p f, p the token's position, f the pair's turns
 // per position: y_a = A (a cos - b sin), y_b = A (b cos + a sin). The turns p f are formed in 64
 // bits and only their fraction goes on: at p = 10^6 an fp32 product would be off by 0.06 turns.
-// A workgroup takes 1 to 4 tokens and all or a share of their rows. It forms each token's
+// A workgroup takes 1 to 16 tokens and all or a share of their rows. It forms each token's
 // cosines and sines once, in LDS, while its rows are on their way; then every lane turns 16
 // elements, two 16-byte chunks that hold whole pairs in either layout. A, cos and sin are joined
 // in 64 bits and rounded to fp32; products and sums round one by one (no fused ones), so the
@@ -21,7 +21,7 @@ namespace ef {
 
 namespace {
 
-constexpr int kMaxPer = 4;
+constexpr int kMaxPer = 16;
 
 struct Chunks {
   uint32_t a[4], b[4];  // elements 0 .. 7 and 8 .. 15 of a lane, bf16 pairs
@@ -46,7 +46,7 @@ __device__ __forceinline__ uint32_t codes4(const float* x, float inv) {
   return u;
 }
 
-template <int D, bool E4M3>
+template <int D, bool E4M3, bool ONCE>
 __global__ __launch_bounds__(256) void rows_kernel(RowsParams a) {
 #pragma clang fp contract(off)
   constexpr int LPR = D / 16;  // lanes of a row
@@ -59,22 +59,24 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsParams a) {
   const int per = min(a.per, a.T - t0);
   const int rows = a.Hq + 2 * a.Hkv;
 
-  // Wave w finds token t0 + w.
-  if (wave < per) {
-    const int t = t0 + wave;
-    long long p;
-    int b = 0;
-    if (a.positions != nullptr) {
-      p = a.positions[t];
-    } else {
-      b = find_sequence(a.starts, a.B, a.T, t);
-      if (b >= a.B) b = -1;
-      // len_b - n_b + (t - start_b), where n_b = start_(b + 1) - start_b
-      p = b < 0 ? 0 : (long long)a.lengths[b] + t - sequence_start(a.starts, b + 1, a.B, a.T);
-    }
-    if (lane == 0) {
-      pos[wave] = p;
-      seq[wave] = b;
+  // The tokens' places, one to a lane: starts ascend, so a token's sequence is the first token's
+  // or one behind it.
+  if (wave == 0) {
+    int b = a.positions != nullptr ? 0 : find_sequence(a.starts, a.B, a.T, t0);
+    if (lane < per) {
+      const int t = t0 + lane;
+      long long p = 0;
+      if (a.positions != nullptr) {
+        p = a.positions[t];
+      } else {
+        int end = 0;  // first row behind the sequence
+        while (b < a.B && (end = sequence_start(a.starts, b + 1, a.B, a.T)) <= t) ++b;
+        if (b >= a.B) b = -1;
+        // len_b - n_b + (t - start_b), where n_b = end_b - start_b
+        if (b >= 0) p = (long long)a.lengths[b] + t - end;
+      }
+      pos[lane] = p;
+      seq[lane] = b;
     }
   }
   // This lane's first row goes out for its elements before the angles are formed.
@@ -97,6 +99,14 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsParams a) {
   auto fetch = [&](const uint16_t* p, u32x4_t& x, u32x4_t& y) {
     x = *reinterpret_cast<const u32x4_t*>(p + o1);
     y = *reinterpret_cast<const u32x4_t*>(p + o2);
+  };
+  // Outputs that no cache can hold for their reader stream past them.
+  auto store = [&](auto v, auto* p) {
+    auto* const q = reinterpret_cast<decltype(v)*>(p);
+    if constexpr (ONCE)
+      __builtin_nontemporal_store(v, q);
+    else
+      *q = v;
   };
   u32x4_t x = {0u, 0u, 0u, 0u}, y = x;
   int n = 0, h = 0;
@@ -184,8 +194,8 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsParams a) {
         char* const row = (isk ? a.c.k : a.c.v) + cell * D;
         const u32x2_t c1 = {codes4(u, inv), codes4(u + 4, inv)};
         const u32x2_t c2 = {codes4(w, inv), codes4(w + 4, inv)};
-        *reinterpret_cast<u32x2_t*>(row + o1) = c1;
-        *reinterpret_cast<u32x2_t*>(row + o2) = c2;
+        store(c1, row + o1);
+        store(c2, row + o2);
         if (ch == 0) (isk ? a.c.k_scale : a.c.v_scale)[cell] = s;
       }
     } else if (to != nullptr) {
@@ -195,8 +205,8 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsParams a) {
         p1[i] = pack_bf16x2(u[2 * i], u[2 * i + 1]);
         p2[i] = pack_bf16x2(w[2 * i], w[2 * i + 1]);
       }
-      *reinterpret_cast<u32x4_t*>(to + o1) = p1;
-      *reinterpret_cast<u32x4_t*>(to + o2) = p2;
+      store(p1, to + o1);
+      store(p2, to + o2);
     }
   }
 }
@@ -204,10 +214,9 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsParams a) {
 template <int D>
 hipError_t launch_d(const RowsParams& a, bool e4m3, hipStream_t stream) {
   const dim3 grid((unsigned)((a.T + a.per - 1) / a.per) * a.blocks);
-  if (e4m3)
-    hipLaunchKernelGGL((rows_kernel<D, true>), grid, dim3(256), 0, stream, a);
-  else
-    hipLaunchKernelGGL((rows_kernel<D, false>), grid, dim3(256), 0, stream, a);
+  auto* const kernel = e4m3 ? (a.once ? rows_kernel<D, true, true> : rows_kernel<D, true, false>)
+                            : (a.once ? rows_kernel<D, false, true> : rows_kernel<D, false, false>);
+  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
