@@ -45,8 +45,8 @@ class Pages:
     """A cache with random rows where sequences have keys, NaN everywhere else, and its values in
     64 bits."""
 
-    def __init__(self, seed, H, page, D, lengths, e4m3, capacities=None, kv=None):
-        self.pages, self.table = make_table(seed, page, capacities or lengths)
+    def __init__(self, seed, H, page, D, lengths, e4m3):
+        self.pages, self.table = make_table(seed, page, lengths)
         shape = (self.pages, H, page, D)
         self.values, held = [], []
         live = np.zeros((self.pages, page), bool)
@@ -57,8 +57,6 @@ class Pages:
         live = torch.from_numpy(live)[:, None].expand(self.pages, H, page)
         for i in range(2):
             x = normal(seed + 1 + i, *shape)
-            if kv is not None:
-                x = kv[i](x)
             if e4m3:
                 codes, scales = quantised(x)
                 codes.view(torch.uint8)[~live] = 0x7f
