@@ -7,11 +7,11 @@
 // its rows are loaded at that stride, straight to LDS.
 //
 // Work: a sequence has ceil(G n / 128) row tiles. Where all sequences' tiles do not fill the
-// chip, or one of them has far more keys than its share, keys are cut into parts of C tiles, C
-// taken from the sums over the sequences that every workgroup forms for itself (64 at a time, a
-// wave-wide sum): parts leave states in the workspace and a second kernel joins them, each of a
+// chip, or one of them has far more keys than its share, a sequence's keys are cut into equal
+// parts of at most C tiles, C taken from the sums over the sequences that every workgroup forms for
+// itself (64 at a time, a wave-wide sum): parts leave states in the workspace and a second kernel joins them, each of a
 // tile's P workgroups a P-th of its rows. Up to 64 sequences run in the order of their
-// keys, longest first, and the tiles of one from its last rows on, so that the last workgroups to
+// parts' keys, longest first, and the tiles of one from its last rows on, so that the last workgroups to
 // start are the shortest.
 #include "ef_serve.hpp"
 #include "roll_tiles.hpp"
@@ -138,10 +138,10 @@ struct Unit {
     }
     work = ((long long)__builtin_amdgcn_readfirstlane((int)(work >> 32)) << 32) |
            (unsigned)__builtin_amdgcn_readfirstlane((int)work);
-    C = 0x7fffffff;
+    int most = 0x7fffffff;  // key tiles of a part
     if (a.slots > 0) {
       const int places = rows >= a.fill ? a.fill : max(a.fill - rows, (a.fill + 1) / 2);
-      C = (int)min(max((work + places - 1) / places, (long long)a.least), 0x7fffffffLL);
+      most = (int)min(max((work + places - 1) / places, (long long)a.least), 0x7fffffffLL);
     }
     // The sequence that holds the unit: units of the ones in front of it in `order`.
     int before = 0, slots = 0;
@@ -154,15 +154,17 @@ struct Unit {
           kt = x.key_tiles();
         }
       }
-      const int parts = C == 0x7fffffff ? 1 : (kt + C - 1) / C;
-      const int units = m * max(parts, 1);
+      // As many parts as that takes, of equal sizes.
+      const int parts = max((int)(((unsigned)kt + (unsigned)most - 1) / (unsigned)most), 1);
+      const int each = ((unsigned)kt + parts - 1) / (unsigned)parts;
+      const int units = m * parts;
       const int split = parts > 1 ? units : 0;
       // Units in front of this lane's sequence.
       int front = 0, at = 0;
       if (a.B <= 64) {
         for (int i = 0; i < a.B; ++i) {
-          const int k = __builtin_amdgcn_readlane(kt, i), n = __builtin_amdgcn_readlane(units, i);
-          const bool ahead = k > kt || (k == kt && i < lane);
+          const int k = __builtin_amdgcn_readlane(each, i), n = __builtin_amdgcn_readlane(units, i);
+          const bool ahead = k > each || (k == each && i < lane);
           front += ahead ? n : 0;
         }
       } else {
@@ -177,7 +179,8 @@ struct Unit {
         e.n = __builtin_amdgcn_readlane(x.n, at);
         e.kstart = __builtin_amdgcn_readlane(x.kstart, at);
         e.len = __builtin_amdgcn_readlane(x.len, at);
-        P = max(__builtin_amdgcn_readlane(parts, at), 1);
+        P = __builtin_amdgcn_readlane(parts, at);
+        C = __builtin_amdgcn_readlane(each, at);
         const int tiles = __builtin_amdgcn_readlane(m, at);
         const int in = id - __builtin_amdgcn_readlane(lo, at);
         mt = tiles - 1 - in / P;
