@@ -88,13 +88,14 @@ struct PackedTiles {
 struct Extent {
   int start, n, kstart, len;
   __device__ __forceinline__ void load(const PackedParams& a, int b) {
-    start = sequence_start(a.starts, b, a.B, a.T);
-    n = max(sequence_start(a.starts, b + 1, a.B, a.T) - start, 0);
-    kstart = sequence_start(a.k_starts, b, a.B, a.Tk);
-    len = max(sequence_start(a.k_starts, b + 1, a.B, a.Tk) - kstart, 0);
+    const int s0 = a.starts[b], s1 = a.starts[b + 1], k0 = a.k_starts[b], k1 = a.k_starts[b + 1];
+    start = min(max(s0, 0), a.T);
+    n = max(min(max(s1, 0), a.T) - start, 0);
+    kstart = min(max(k0, 0), a.Tk);
+    len = max(min(max(k1, 0), a.Tk) - kstart, 0);
   }
   __device__ __forceinline__ int row_tiles(const PackedParams& a) const {
-    return (int)(((long long)n * a.G + kRows - 1) / kRows);
+    return (int)(((unsigned)(n * a.G) + kRows - 1) / kRows);  // (n G is below 2^31 - 128)
   }
   __device__ __forceinline__ int key_tiles() const { return max((len + 63) / 64, 1); }
   // Keys that some row of row tile mt sees.
@@ -118,7 +119,7 @@ struct Unit {
   __device__ __forceinline__ bool find(const PackedParams& a, int id) {
     const int lane = threadIdx.x & 63;
     // Sums over the sequences.
-    long long work = 0;
+    float work = 0.f;
     int rows = 0;
     Extent x;
     int m = 0, kt = 0;
@@ -130,18 +131,15 @@ struct Unit {
         kt = x.key_tiles();
       }
       rows += __builtin_amdgcn_readlane(wave_scan(m), 63);
-      // (products below 2^31 x 2^25)
-      long long y = (long long)m * kt;
-#pragma unroll
-      for (int off = 1; off < 64; off *= 2) y += __shfl_xor(y, off, 64);
-      work += y;
+      work += wave_sum((float)m * (float)kt);
     }
-    work = ((long long)__builtin_amdgcn_readfirstlane((int)(work >> 32)) << 32) |
-           (unsigned)__builtin_amdgcn_readfirstlane((int)work);
     int most = 0x7fffffff;  // key tiles of a part
     if (a.slots > 0) {
       const int places = rows >= a.fill ? a.fill : max(a.fill - rows, (a.fill + 1) / 2);
-      most = (int)min(max((work + places - 1) / places, (long long)a.least), 0x7fffffffLL);
+      // At least work / places, for all that fp32 rounds: the states' room counts on it. (The same
+      // in every workgroup of both launches.)
+      most = (int)fminf(work * 1.001f / (float)places + 1.f, 2e9f);
+      most = max(__builtin_amdgcn_readfirstlane(most), a.least);
     }
     // The sequence that holds the unit: units of the ones in front of it in `order`.
     int before = 0, slots = 0;
@@ -161,7 +159,7 @@ struct Unit {
       const int split = parts > 1 ? units : 0;
       // Units in front of this lane's sequence.
       int front = 0, at = 0;
-      if (a.B <= 64) {
+      if (a.B <= 64 && rows > a.fill) {  // (in one round the order does not matter)
         for (int i = 0; i < a.B; ++i) {
           const int k = __builtin_amdgcn_readlane(each, i), n = __builtin_amdgcn_readlane(units, i);
           const bool ahead = k > each || (k == each && i < lane);
@@ -183,10 +181,10 @@ struct Unit {
         C = __builtin_amdgcn_readlane(each, at);
         const int tiles = __builtin_amdgcn_readlane(m, at);
         const int in = id - __builtin_amdgcn_readlane(lo, at);
-        mt = tiles - 1 - in / P;
-        p = in % P;
+        mt = tiles - 1 - (int)((unsigned)in / (unsigned)P);
+        p = (int)((unsigned)in % (unsigned)P);
         slot = slots + __builtin_amdgcn_readlane(sfront, at) + in;
-        return P == 1 || slot < a.slots;  // (always, where starts ascend)
+        return P == 1 || (unsigned)slot < (unsigned)a.slots;  // (always, where starts ascend)
       }
       before += __builtin_amdgcn_readlane(wave_scan(units), 63);
       slots += __builtin_amdgcn_readlane(wave_scan(split), 63);
@@ -214,7 +212,7 @@ void attn_packed_kernel(PackedParams a) {
   const int rows = e.n * a.G;
   const int r = u.mt * kRows + wave * 32 + ql;
   const bool valid = r < rows;
-  const int i = valid ? r / a.G : 0, g = valid ? r % a.G : 0;
+  const int i = valid ? (unsigned)r / (unsigned)a.G : 0, g = valid ? r - i * a.G : 0;
   const size_t orow = ((size_t)(e.start + i) * a.Hq + (size_t)hk * a.G + g) * D;
 
   PackedTiles<D> tl;

@@ -1115,22 +1115,23 @@ def cache_write(cache: PagedCache, k, v, table, lengths, starts=None, q=None,
     bf16, i32 = torch.bfloat16, torch.int32
     dev = k.get_device()
     pages, H, page, D = cache.shape
+    shape, places = k.shape, table.shape
     if not (k.dtype is bf16 and v.dtype is bf16 and table.dtype is i32 and lengths.dtype is i32 and
             k.is_contiguous() and v.is_contiguous() and table.is_contiguous() and
             lengths.is_contiguous() and dev >= 0 and v.get_device() == dev and
             table.get_device() == dev and lengths.get_device() == dev and
-            cache.k.get_device() == dev and k.dim() == 3 and k.shape == v.shape and
-            k.shape[1] == H and k.shape[2] == D and table.dim() == 2 and lengths.dim() == 1 and
-            lengths.shape[0] == table.shape[0] > 0 and
-            (k.shape[0] % table.shape[0] == 0 if starts is None else
+            cache.k.get_device() == dev and len(shape) == 3 and shape == v.shape and
+            shape[1] == H and shape[2] == D and len(places) == 2 and
+            lengths.shape == places[:1] and places[0] > 0 and
+            (shape[0] % places[0] == 0 if starts is None else
              starts.dtype is i32 and starts.is_contiguous() and starts.get_device() == dev and
-             starts.dim() == 1 and starts.shape[0] == table.shape[0] + 1)):
+             starts.dim() == 1 and starts.shape[0] == places[0] + 1)):
         _rows3(k, "k")
         _rows3(v, "v", k, k.shape)
         _same_cache(cache, k, k.shape[2], k.shape[1])
         _table_and_lengths(table, lengths, starts, k.shape[0], k)
-    T = k.shape[0]
-    B, width = table.shape
+    T = shape[0]
+    B, width = places
     Hq, qp, op = 0, None, None
     if q is not None:
         o = q if q_out is None else q_out
