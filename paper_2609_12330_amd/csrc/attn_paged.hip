@@ -15,10 +15,12 @@
 // 8-bit caches: e4m3 codes are exact in bf16, and scales factor out of both products, a key's of
 // its score and a value's of its weight (16 keys at a time, four floats a lane).
 //
-// Work: the keys of all sequences, in steps of 64, make one list for each kv head (and row
+// Work: the keys of all sequences, in units of 64, make one list for each kv head (and row
 // tile), which W workgroups cut into equal runs, whatever the lengths. A run holds the end of
 // one sequence, whole ones, and the beginning of another; what is cut leaves a state in the
-// workspace (two slots a workgroup), and a second kernel joins the states of a row.
+// workspace (two slots a workgroup), and the last of a row's parts joins them, or a second kernel.
+// (Workgroups of their own for sequences of equal lengths: 8 of 8192 keys, 8 tokens each, 60.5 ->
+// 56.3 us, but 0.2 to 0.4 us more for every other call; not kept.)
 #include "ef_device.hpp"
 #include "ef_serve.hpp"
 #include "group_combine.hpp"
@@ -32,6 +34,7 @@ constexpr int kUnit = 64;             // keys of a unit of work
 // Bytes of keys that a sequence counts beside its own: what a workgroup takes from one sequence to the
 // next (rows, table, the first loads' way, the join of its waves).
 constexpr int kExtraBytes = 64 * 1024;
+constexpr int kWideChannels = 32;     // of a row that a workgroup joins from hundreds of parts
 constexpr float kHeadroom = 8.f;      // base-2 headroom before the reference moves
 constexpr int kStageBytes = 8192;     // keys, and values, of a wave's step
 // A value that is the same in all lanes, for the compiler to see.
@@ -41,7 +44,6 @@ template <int N>
 __device__ __forceinline__ void wait_loads() {
   __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
 }
-constexpr int NT = 2;                 // cache policy of loads: non-temporal
 
 typedef int v2i __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
@@ -98,20 +100,22 @@ struct Sequences {
   }
 };
 
-// Parts p0 .. p1 - 1 of a row joined by one wave: the value (D / 4 lanes, four channels each, the
-// same in every group of them) and the sum against the reference M (base-2 units).
+// Parts p0 .. p1 - 1 of a row joined by one wave: the value's channels c0 .. c0 + CH - 1 (CH / 4
+// lanes, four each, the same in every group of them) and the sum against the reference M (base-2
+// units).
 struct Joined {
   floatx4 x;
   float M, L;
 };
-template <int D, int BATCH, bool SHARED, class State>
-__device__ __forceinline__ Joined join_parts(const PagedParams& a, int p0, int p1, State state) {
-  constexpr int LPS = D / 4, SPL = 64 / LPS;  // lanes of a state, states of a wave-wide load
+template <int D, int CH, int BATCH, bool SHARED, class State>
+__device__ __forceinline__ Joined join_parts(const PagedParams& a, int p0, int p1, int c0,
+                                             State state) {
+  constexpr int LPS = CH / 4, SPL = 64 / LPS;  // lanes of a state, states of a wave-wide load
   const int lane = threadIdx.x & 63, grp = lane / LPS, ch = lane % LPS;
   const __amdgpu_buffer_rsrc_t rs =
       __builtin_amdgcn_make_buffer_rsrc(a.ws_acc, (short)0, -1, 0x00020000);
   auto value = [&](int p) -> floatx4 {
-    const size_t at = state(p) * D + 4 * ch;
+    const size_t at = state(p) * D + c0 + 4 * ch;
     if constexpr (SHARED) return __builtin_bit_cast(floatx4, load16_dev(rs, (int)(at * 4)));
     return *reinterpret_cast<const floatx4*>(a.ws_acc + at);
   };
@@ -154,10 +158,10 @@ __device__ __forceinline__ Joined join_parts(const PagedParams& a, int p0, int p
     for (int e = 0; e < 4; ++e) j.x[e] += shfl_xor(j.x[e], off);
   return j;
 }
-template <int D>
+template <int CH>
 __device__ __forceinline__ void store_joined(const Joined& j, float inv, uint16_t* o) {
   const int lane = threadIdx.x & 63;
-  if (lane >= D / 4) return;
+  if (lane >= CH / 4) return;
   const u32x2_t p = {pack_bf16x2(j.x[0] * inv, j.x[1] * inv),
                      pack_bf16x2(j.x[2] * inv, j.x[3] * inv)};
   *reinterpret_cast<u32x2_t*>(o + 4 * lane) = p;
@@ -165,7 +169,7 @@ __device__ __forceinline__ void store_joined(const Joined& j, float inv, uint16_
 
 // (A function beside the kernel: the host's compiler reads a kernel's body too, and does not know
 // buffers.)
-template <int D, bool E4M3, int RT>
+template <int D, bool E4M3, int RT, int NT>
 __device__ __forceinline__ void attend_pages(const PagedParams& a) {
   using G = Geo<D, E4M3>;
   constexpr int ROWS = 16 * RT, KT = G::KT, DT = G::DT;
@@ -647,6 +651,7 @@ __device__ __forceinline__ void attend_pages(const PagedParams& a) {
         store_dev(a.ws_l + slot * ROWS + r, L);
       }
     }
+    // The sequence's first workgroup, and how many have keys of it.
     const int w0 = (unsigned)first / (unsigned)T;
     const int P = (unsigned)(first + units - 1) / (unsigned)T - w0 + 1;
     if (RT == 2 || a.counters == nullptr) {
@@ -661,7 +666,7 @@ __device__ __forceinline__ void attend_pages(const PagedParams& a) {
           const size_t slot0 = ((size_t)head * a.W + w0) * 2;
           Joined j = {{0.f, 0.f, 0.f, 0.f}, 0.f, 0.f};
           if (ticket == (unsigned)(P - 1))
-            j = join_parts<D, 8, true>(a, 0, P, [&](int p) {
+            j = join_parts<D, D, 8, true>(a, 0, P, 0, [&](int p) {
               return (slot0 + 2 * p + (p == 0 ? 1 : 0)) * ROWS + r;
             });
           // (A counter that was not zero: NaN.)
@@ -680,19 +685,21 @@ __device__ __forceinline__ void attend_pages(const PagedParams& a) {
   }
 }
 
-template <int D, bool E4M3, int RT>
+// NT: cache policy of the loads of keys and values.
+template <int D, bool E4M3, int RT, int NT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 void attn_paged_kernel(PagedParams a) {
-  attend_pages<D, E4M3, RT>(a);
+  attend_pages<D, E4M3, RT, NT>(a);
 }
 
-// Joins the parts of a row that several workgroups share: WPR waves a row, each its share of the
-// parts.
-template <int D, int ROWS, int WPR>
+// Joins the parts of a row that several workgroups share: a wave a row, or (WIDE) four waves for 32
+// channels of it, each a quarter of the parts.
+template <int D, int ROWS, bool WIDE>
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedParams a, int tiles) {
-  constexpr int RPW = 4 / WPR;  // rows of a workgroup
+  constexpr int CH = WIDE ? kWideChannels : D;  // channels of a wave
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r = (int)(blockIdx.x % tiles) * RPW + wave / WPR;
+  const int x = (int)(blockIdx.x % tiles);
+  const int r = WIDE ? x / (D / CH) : x * 4 + wave, c0 = WIDE ? x % (D / CH) * CH : 0;
   const int head = (int)(blockIdx.x / tiles % a.heads);
   const int b = (int)(blockIdx.x / tiles / a.heads);
   const int mt = head % a.mtiles, hk = head / a.mtiles;
@@ -702,14 +709,15 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedParams a, int t
   const int row = mt * ROWS + r;
   // (Without rows in this tile nothing wrote `part`. All waves of a row end here, or none.)
   if (r >= ROWS || row >= min(n, a.max_queries) * a.G || part.y < 2) return;
-  const int P = part.y, x = wave % WPR;
+  const int P = part.y;
   const size_t slot0 = ((size_t)head * a.W + part.x) * 2;
-  Joined j = join_parts<D, 8, false>(a, P * x / WPR, P * (x + 1) / WPR, [&](int p) {
+  Joined j = join_parts<D, CH, 8, false>(a, WIDE ? P * wave / 4 : 0, WIDE ? P * (wave + 1) / 4 : P,
+                                         c0, [&](int p) {
     return (slot0 + 2 * p + (p == 0 ? 1 : 0)) * ROWS + r;
   });
-  if constexpr (WPR > 1) {
-    __shared__ float sx[4][D], sm[4], sl[4];
-    if (lane < D / 4) *reinterpret_cast<floatx4*>(&sx[wave][4 * lane]) = j.x;
+  if constexpr (WIDE) {
+    __shared__ float sx[4][CH], sm[4], sl[4];
+    if (lane < CH / 4) *reinterpret_cast<floatx4*>(&sx[wave][4 * lane]) = j.x;
     if (lane == 0) {
       sm[wave] = j.M;
       sl[wave] = j.L;
@@ -723,36 +731,47 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedParams a, int t
     for (int y = 0; y < 4; ++y) {
       const float wt = exp2_fast(sm[y] - ref);
       j.L = fmaf(wt, sl[y], j.L);
-      if (lane < D / 4)
+      if (lane < CH / 4)
 #pragma unroll
         for (int e = 0; e < 4; ++e) j.x[e] = fmaf(wt, sx[y][4 * lane + e], j.x[e]);
     }
   }
-  store_joined<D>(j, j.L == 0.f ? 0.f : 1.f / j.L,
-                  a.o + ((size_t)(start + row / a.G) * a.Hq + (size_t)hk * a.G + row % a.G) * D);
+  store_joined<CH>(
+      j, j.L == 0.f ? 0.f : 1.f / j.L,
+      a.o + ((size_t)(start + row / a.G) * a.Hq + (size_t)hk * a.G + row % a.G) * D + c0);
 }
 
-template <int D, bool E4M3, int RT>
+constexpr int kOnce = 2, kAgain = 0;  // non-temporal, cached
+
+template <int D, bool E4M3, int RT, int NT>
 hipError_t launch(const PagedParams& a, hipStream_t stream) {
-  hipLaunchKernelGGL((attn_paged_kernel<D, E4M3, RT>), dim3((unsigned)a.heads * a.W), dim3(256), 0,
-                     stream, a);
+  hipLaunchKernelGGL((attn_paged_kernel<D, E4M3, RT, NT>), dim3((unsigned)a.heads * a.W), dim3(256),
+                     0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.counters != nullptr) return e;
-  // A wave a row where the parts may be few, four where there may be hundreds.
+  // A wave a row where the parts may be few; where there may be hundreds, four waves for every 32
+  // channels of a row.
   const int rows = a.mtiles > 1 ? 16 * RT : a.rows;
   const bool wide = a.W > 128;
-  const int tiles = wide ? rows : (rows + 3) / 4;
+  const int tiles = wide ? rows * (D / kWideChannels) : (rows + 3) / 4;
   const dim3 grid((unsigned)a.B * a.heads * tiles);
   if (wide)
-    hipLaunchKernelGGL((paged_combine_kernel<D, 16 * RT, 4>), grid, dim3(256), 0, stream, a, tiles);
+    hipLaunchKernelGGL((paged_combine_kernel<D, 16 * RT, true>), grid, dim3(256), 0, stream, a,
+                       tiles);
   else
-    hipLaunchKernelGGL((paged_combine_kernel<D, 16 * RT, 1>), grid, dim3(256), 0, stream, a, tiles);
+    hipLaunchKernelGGL((paged_combine_kernel<D, 16 * RT, false>), grid, dim3(256), 0, stream, a,
+                       tiles);
   return hipGetLastError();
 }
 
 template <int D, bool E4M3>
 hipError_t launch_rt(const PagedParams& a, hipStream_t stream) {
-  return a.rt == 1 ? launch<D, E4M3, 1>(a, stream) : launch<D, E4M3, 2>(a, stream);
+  if (a.rt == 1) return launch<D, E4M3, 1, kOnce>(a, stream);
+  // Several row tiles read the same keys, out of the L2 cache but for the first (8 sequences of 16
+  // tokens of 64/8 heads of 128 over 8192 keys, non-temporal / cached 137 / 94 us; one row tile
+  // reads them once, 64 sequences of one token of 32/8 heads of 64 over 4096 85 / 94).
+  return a.mtiles == 1 ? launch<D, E4M3, 2, kOnce>(a, stream)
+                       : launch<D, E4M3, 2, kAgain>(a, stream);
 }
 
 template <int D>

@@ -96,8 +96,12 @@ constexpr int kMostWgs = 2048;
 static_assert(kMostWgs * 64 <= ef::kCounterRegionBytes, "a counter for every workgroup");
 constexpr int kJoinElems = 1024;
 constexpr int kJoinParts = 128;
+constexpr int kLeastKeys = 128;  // keys of a part, at least
 
-ef_status paged_plan(PagedPlan& p, int T, int B, int Hq, int Hkv, int D, int max_queries) {
+// `positions`: the table's, which bound the parts of a row (0 for the workspace's size, which does
+// not depend on them).
+ef_status paged_plan(PagedPlan& p, int T, int B, int Hq, int Hkv, int D, int max_queries,
+                     long long positions) {
   const ef_status st = check_heads(T, B, Hq, Hkv, D);
   if (st != EF_OK) return st;
   if (max_queries < 0) return EF_ERR_INVALID_SHAPE;
@@ -112,8 +116,9 @@ ef_status paged_plan(PagedPlan& p, int T, int B, int Hq, int Hkv, int D, int max
   p.W = std::max(1, std::max(kFillWgs / p.heads, std::min(B, kMostWgs / p.heads)));
   if ((long long)p.heads * p.W > kMaxGroups) return EF_ERR_INVALID_SHAPE;
   // The last of a row's parts joins them in the same launch where these are few (see below).
-  p.fused = rows * D <= kJoinElems && p.W <= kJoinParts && p.heads * p.W <= kMostWgs;
-  if (!p.fused && (long long)B * p.heads * std::min(rows, tile) > kMaxGroups)
+  const long long parts = std::min<long long>(p.W, positions / kLeastKeys + 2);
+  p.fused = rows * D <= kJoinElems && parts <= kJoinParts && p.heads * p.W <= kMostWgs;
+  if (!p.fused && (long long)B * p.heads * std::min(rows, tile) * 4 > kMaxGroups)
     return EF_ERR_INVALID_SHAPE;
   const size_t states = (size_t)p.heads * p.W * 2 * tile;
   p.parts_off = ef::kCounterRegionBytes;
@@ -254,7 +259,7 @@ ef_status ef_cache_read(const void* k_cache, const void* v_cache, const float* k
 
 size_t ef_attention_paged_workspace_size(int T, int B, int Hq, int Hkv, int D, int max_queries) {
   PagedPlan p{};
-  if (paged_plan(p, T, B, Hq, Hkv, D, max_queries) != EF_OK || B == 0) return 0;
+  if (paged_plan(p, T, B, Hq, Hkv, D, max_queries, 0) != EF_OK || B == 0) return 0;
   return p.bytes;
 }
 
@@ -265,9 +270,9 @@ ef_status ef_attention_paged(const void* q, const void* k_cache, const void* v_c
                              int format, float scale, void* workspace, size_t workspace_bytes,
                              void* stream) {
   PagedPlan p{};
-  ef_status st = paged_plan(p, T, B, Hq, Hkv, D, max_queries);
+  ef_status st = check_pages(pages, page, width, format);
   if (st != EF_OK) return st;
-  st = check_pages(pages, page, width, format);
+  st = paged_plan(p, T, B, Hq, Hkv, D, max_queries, (long long)width * page);
   if (st != EF_OK) return st;
   // The units of work of a head are counted in 32 bits.
   if ((long long)B * ((long long)width * page / 64 + 32) >= (1LL << 31))

@@ -333,13 +333,13 @@ def test_streams_and_workspaces():
         torch.cuda.synchronize()
 
 
-@pytest.mark.parametrize("H,counts", [(2, False), (8, True)])
-def test_counter_that_was_not_zero(H, counts):
-    """From the number of parts on: NaN rows, and the region cleared makes it good again. (With 2 kv
-    heads a row may have hundreds of parts, which a second launch joins without counters.)"""
+@pytest.mark.parametrize("Hq,H,counts", [(8, 2, True), (16, 8, True), (32, 2, False)])
+def test_counter_that_was_not_zero(Hq, H, counts):
+    """From the number of parts on: NaN rows, and the region cleared makes it good again. (The parts
+    of 16 rows of a kv head are joined by a second launch, without counters.)"""
     announce(f"paged counters {H}")
     p = Pages(54, H, 16, 128, [3000], False)
-    q = normal(55, 1, 2 * H if counts else 8, 128).cuda()
+    q = normal(55, 1, Hq, 128).cuda()
     ws = ef.make_paged_workspace(q, p.cache, 1, 1)
     want = ef.attention_paged(q, p.cache, p.dev_table, ints([3000]), workspace=ws)
     ef.workspace_counters(ws)[:] = 1000
