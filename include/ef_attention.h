@@ -575,9 +575,9 @@ size_t ef_attention_shared_prefix_workspace_size(int B, int Hq, int Hkv, int Sq,
  * to the gradient of x.
  *   x, out    : [T][H][D] bf16; they may be the same buffer, but not overlap otherwise.
  *   positions : [T] int32, any value.
- *   turns     : [rot / 2] double, device, 16-byte aligned: turns (of 2 pi) per position. Angles are formed in 64
- *               bits, so far positions lose nothing; amplitude cos and amplitude sin are
- *               rounded to fp32, and so is each product and sum, and the result to bf16.
+ *   turns     : [rot / 2] double, device, 16-byte aligned: turns (of 2 pi) per position. Angles
+ *               are formed in 64 bits, so far positions lose nothing; amplitude cos and amplitude
+ *               sin are rounded to fp32, and so is each product and sum, and the result to bf16.
  *   rot       : a multiple of 16, 16 .. D.
  * Errors: EF_ERR_INVALID_ROPE; others as for ef_attention_fwd.
  */

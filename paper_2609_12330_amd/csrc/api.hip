@@ -362,7 +362,7 @@ const char* ef_status_string(int status) {
              "sink_blocks + local_blocks, sink_blocks >= 0, local_blocks >= 1, new_keys >= 0";
     case EF_ERR_INVALID_PAGES:
       return "page must be 16, 32, 64, 128 or 256 with at least one page, a table width >= 0 of "
-             "fewer than 2^31 positions, and a cache format of bf16 or e4m3";
+             "fewer than 2^31 - 4096 positions, and a cache format of bf16 or e4m3";
     case EF_ERR_INVALID_ROPE:
       return "rot must be a multiple of 16 from 16 to D and amplitude finite";
     default: return "unknown status";

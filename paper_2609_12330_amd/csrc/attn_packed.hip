@@ -7,12 +7,20 @@
 // its rows are loaded at that stride, straight to LDS.
 //
 // Work: a sequence has ceil(G n / 128) row tiles. Where all sequences' tiles do not fill the
-// chip, or one of them has far more keys than its share, a sequence's keys are cut into equal
-// parts of at most C tiles, C taken from the sums over the sequences that every workgroup forms for
-// itself (64 at a time, a wave-wide sum): parts leave states in the workspace and a second kernel joins them, each of a
-// tile's P workgroups a P-th of its rows. Up to 64 sequences run in the order of their
-// parts' keys, longest first, and the tiles of one from its last rows on, so that the last workgroups to
-// start are the shortest.
+// chip, or one of them has far more keys than its share, a sequence's keys are cut into equal parts
+// of at most C tiles, C taken from the sums over the sequences that every workgroup forms for
+// itself (64 at a time, a wave-wide sum): parts leave states in the workspace and a second kernel
+// joins them. Up to 64 sequences run in the
+// order of their parts' keys, longest first, and the tiles of one from its last rows on, so that
+// the last workgroups to start are the shortest.
+//
+// What bounds it: the matrix core and the power limit, as for the prefill kernel: 16 prompts of 101
+// to 4096 tokens of 32/8 heads of 128 (774 GFLOP) 785 to 800 us, 0.97 to 0.99 PFLOP/s; 16 equal ones of
+// 2048 603 us, where the prefill kernel on padded tensors takes 620. Chunks of 700 and 1500
+// tokens of 64/8 heads of 64 over 9001 and 16001 keys (382 GFLOP) 410 to 430 us, 0.89 to 0.93: 1104
+// workgroups of two lengths on 512 places. Finer parts lose more than they even out: at most a half
+// / a third / a quarter of a place's share 410 -> 440 / 490 / 480 us. Three short prompts 11.4 us:
+// round trips (sequences, first tiles, rows) and five key tiles.
 #include "ef_serve.hpp"
 #include "roll_tiles.hpp"
 #include "wave_ops.hpp"
@@ -106,6 +114,59 @@ struct Extent {
   }
 };
 
+// 64 sequences, one to a lane: their row tiles, key tiles, and how the keys are cut.
+struct Cut {
+  Extent x;
+  int m, kt;         // row tiles, key tiles
+  int parts, each;   // equal parts of the keys, key tiles of one
+  int units, split;  // workgroups, and those that leave a state
+  __device__ __forceinline__ void load(const PackedParams& a, int b0) {
+    const int b = b0 + (int)(threadIdx.x & 63);
+    m = kt = 0;
+    if (b < a.B) {
+      x.load(a, b);
+      m = x.row_tiles(a);
+      kt = x.key_tiles();
+    }
+  }
+  __device__ __forceinline__ void cut(int most) {
+    parts = max((int)(((unsigned)kt + (unsigned)most - 1) / (unsigned)most), 1);
+    each = ((unsigned)kt + parts - 1) / (unsigned)parts;
+    units = m * parts;
+    split = parts > 1 ? units : 0;
+  }
+};
+
+// Most key tiles of a part, and the row tiles of all sequences. The same in every workgroup of both
+// launches. `c` is left with the last 64 sequences.
+__device__ __forceinline__ int most_tiles(const PackedParams& a, Cut& c, int& rows) {
+  float work = 0.f;
+  rows = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    c.load(a, b0);
+    rows += __builtin_amdgcn_readlane(wave_scan(c.m), 63);
+    work += wave_sum((float)c.m * (float)c.kt);
+  }
+  if (a.slots == 0) return 0x7fffffff;
+  const int places = rows >= a.fill ? a.fill : max(a.fill - rows, (a.fill + 1) / 2);
+  // At least work / places, for all that fp32 rounds: the states' room counts on it.
+  const int most = (int)fminf(work * 1.001f / (float)places + 1.f, 2e9f);
+  return max(__builtin_amdgcn_readfirstlane(most), a.least);
+}
+
+// States of a kv head that the call makes.
+__device__ __forceinline__ int count_states(const PackedParams& a) {
+  Cut c;
+  int rows, all = 0;
+  const int most = most_tiles(a, c, rows);
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    if (a.B > 64) c.load(a, b0);
+    c.cut(most);
+    all += __builtin_amdgcn_readlane(wave_scan(c.split), 63);
+  }
+  return min(max(all, 0), a.slots);
+}
+
 // What workgroup `id` of a kv head does.
 struct Unit {
   Extent e;
@@ -118,76 +179,45 @@ struct Unit {
   template <bool SLOTS>
   __device__ __forceinline__ bool find(const PackedParams& a, int id) {
     const int lane = threadIdx.x & 63;
-    // Sums over the sequences.
-    float work = 0.f;
-    int rows = 0;
-    Extent x;
-    int m = 0, kt = 0;
+    Cut c;
+    int rows;
+    const int most = most_tiles(a, c, rows);
+    int before = 0, slots = 0;  // of the sequences in front of these 64
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-      m = kt = 0;
-      if (b0 + lane < a.B) {
-        x.load(a, b0 + lane);
-        m = x.row_tiles(a);
-        kt = x.key_tiles();
-      }
-      rows += __builtin_amdgcn_readlane(wave_scan(m), 63);
-      work += wave_sum((float)m * (float)kt);
-    }
-    int most = 0x7fffffff;  // key tiles of a part
-    if (a.slots > 0) {
-      const int places = rows >= a.fill ? a.fill : max(a.fill - rows, (a.fill + 1) / 2);
-      // At least work / places, for all that fp32 rounds: the states' room counts on it. (The same
-      // in every workgroup of both launches.)
-      most = (int)fminf(work * 1.001f / (float)places + 1.f, 2e9f);
-      most = max(__builtin_amdgcn_readfirstlane(most), a.least);
-    }
-    // The sequence that holds the unit: units of the ones in front of it in `order`.
-    int before = 0, slots = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-      if (a.B > 64) {
-        m = kt = 0;
-        if (b0 + lane < a.B) {
-          x.load(a, b0 + lane);
-          m = x.row_tiles(a);
-          kt = x.key_tiles();
-        }
-      }
-      // As many parts as that takes, of equal sizes.
-      const int parts = max((int)(((unsigned)kt + (unsigned)most - 1) / (unsigned)most), 1);
-      const int each = ((unsigned)kt + parts - 1) / (unsigned)parts;
-      const int units = m * parts;
-      const int split = parts > 1 ? units : 0;
+      if (a.B > 64) c.load(a, b0);
+      c.cut(most);
       // Units in front of this lane's sequence.
-      int front = 0, at = 0;
+      int front = 0;
       if (a.B <= 64 && rows > a.fill) {  // (in one round the order does not matter)
         for (int i = 0; i < a.B; ++i) {
-          const int k = __builtin_amdgcn_readlane(each, i), n = __builtin_amdgcn_readlane(units, i);
-          const bool ahead = k > each || (k == each && i < lane);
-          front += ahead ? n : 0;
+          const int k = __builtin_amdgcn_readlane(c.each, i);
+          const int n = __builtin_amdgcn_readlane(c.units, i);
+          front += k > c.each || (k == c.each && i < lane) ? n : 0;
         }
       } else {
-        front = wave_scan(units) - units;
+        front = wave_scan(c.units) - c.units;
       }
-      const int sfront = wave_scan(split) - split;
+      const int sfront = wave_scan(c.split) - c.split;
       const int lo = SLOTS ? slots + sfront : before + front;
-      const auto hit = __builtin_amdgcn_ballot_w64(id >= lo && id < lo + (SLOTS ? split : units));
+      const auto hit =
+          __builtin_amdgcn_ballot_w64(id >= lo && id < lo + (SLOTS ? c.split : c.units));
       if (hit) {
-        at = __builtin_ctzll(hit);
-        e.start = __builtin_amdgcn_readlane(x.start, at);
-        e.n = __builtin_amdgcn_readlane(x.n, at);
-        e.kstart = __builtin_amdgcn_readlane(x.kstart, at);
-        e.len = __builtin_amdgcn_readlane(x.len, at);
-        P = __builtin_amdgcn_readlane(parts, at);
-        C = __builtin_amdgcn_readlane(each, at);
-        const int tiles = __builtin_amdgcn_readlane(m, at);
+        const int at = __builtin_ctzll(hit);
+        e.start = __builtin_amdgcn_readlane(c.x.start, at);
+        e.n = __builtin_amdgcn_readlane(c.x.n, at);
+        e.kstart = __builtin_amdgcn_readlane(c.x.kstart, at);
+        e.len = __builtin_amdgcn_readlane(c.x.len, at);
+        P = __builtin_amdgcn_readlane(c.parts, at);
+        C = __builtin_amdgcn_readlane(c.each, at);
+        const int tiles = __builtin_amdgcn_readlane(c.m, at);
         const int in = id - __builtin_amdgcn_readlane(lo, at);
         mt = tiles - 1 - (int)((unsigned)in / (unsigned)P);
         p = (int)((unsigned)in % (unsigned)P);
         slot = slots + __builtin_amdgcn_readlane(sfront, at) + in;
         return P == 1 || (unsigned)slot < (unsigned)a.slots;  // (always, where starts ascend)
       }
-      before += __builtin_amdgcn_readlane(wave_scan(units), 63);
-      slots += __builtin_amdgcn_readlane(wave_scan(split), 63);
+      before += __builtin_amdgcn_readlane(wave_scan(c.units), 63);
+      slots += __builtin_amdgcn_readlane(wave_scan(c.split), 63);
     }
     return false;
   }
@@ -207,6 +237,11 @@ void attn_packed_kernel(PackedParams a) {
   const int h = lane >> 5, ql = lane & 31;
   const int hk = (int)(blockIdx.x % a.Hkv);
   Unit u;
+  if (blockIdx.x == gridDim.x - 1 && a.slots > 0) {  // one more than the others
+    const int states = count_states(a);
+    if (threadIdx.x == 0) *a.split = states;
+    return;
+  }
   if (!u.find<false>(a, (int)(blockIdx.x / a.Hkv))) return;
   const Extent& e = u.e;
   const int rows = e.n * a.G;
@@ -245,20 +280,24 @@ void attn_packed_kernel(PackedParams a) {
   }
 }
 
-// Joins the parts of split row tiles: workgroup p of a tile's P takes every P-th row, one
-// wave a row, D / 4 lanes a state.
+// Joins the parts of split row tiles: kShares workgroups for each of a tile's P states, one wave a
+// row, D / 4 lanes a state.
+constexpr int kShares = 4;
 template <int D>
 __global__ __launch_bounds__(256) void packed_combine_kernel(PackedParams a) {
   constexpr int LPS = D / 4, SPL = 64 / LPS, BATCH = 8;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int hk = (int)(blockIdx.x % a.Hkv);
+  // (Often nothing is split: the first launch counted the states.)
+  if ((int)(blockIdx.x / kShares / a.Hkv) >= *a.split) return;
+  const int share = (int)(blockIdx.x % kShares);
+  const int hk = (int)(blockIdx.x / kShares % a.Hkv);
   Unit u;
-  if (!u.find<true>(a, (int)(blockIdx.x / a.Hkv))) return;
+  if (!u.find<true>(a, (int)(blockIdx.x / kShares / a.Hkv))) return;
   const int rows = min(kRows, u.e.n * a.G - u.mt * kRows);
   const int P = u.used(a);
   const size_t slot0 = (size_t)hk * a.slots + u.slot - u.p;  // state of part 0
   const int grp = lane / LPS, ch = lane % LPS;
-  for (int r = u.p + u.P * wave; r < rows; r += u.P * 4) {
+  for (int r = u.p + u.P * (4 * share + wave); r < rows; r += u.P * 4 * kShares) {
     auto state = [&](int p) { return (slot0 + p) * kRows + r; };
     float M = kNegInf, L = 0.f;
     floatx4 x = {0.f, 0.f, 0.f, 0.f};
@@ -308,12 +347,12 @@ __global__ __launch_bounds__(256) void packed_combine_kernel(PackedParams a) {
 
 template <int D>
 hipError_t launch_d(const PackedParams& a, hipStream_t stream) {
-  const dim3 grid((unsigned)a.per_head * a.Hkv);
+  const dim3 grid((unsigned)a.per_head * a.Hkv + (a.slots > 0 ? 1 : 0));
   hipLaunchKernelGGL(attn_packed_kernel<D>, grid, dim3(256), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.slots == 0) return e;
-  hipLaunchKernelGGL(packed_combine_kernel<D>, dim3((unsigned)a.slots * a.Hkv), dim3(256), 0,
-                     stream, a);
+  hipLaunchKernelGGL(packed_combine_kernel<D>, dim3((unsigned)a.slots * a.Hkv * kShares), dim3(256),
+                     0, stream, a);
   return hipGetLastError();
 }
 

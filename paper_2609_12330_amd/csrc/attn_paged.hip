@@ -19,8 +19,18 @@
 // tile), which W workgroups cut into equal runs, whatever the lengths. A run holds the end of
 // one sequence, whole ones, and the beginning of another; what is cut leaves a state in the
 // workspace (two slots a workgroup), and the last of a row's parts joins them, or a second kernel.
-// (Workgroups of their own for sequences of equal lengths: 8 of 8192 keys, 8 tokens each, 60.5 ->
-// 56.3 us, but 0.2 to 0.4 us more for every other call; not kept.)
+//
+// What bounds it: HBM where there is work: 32 sequences of 2001 to 32768 keys of 8 heads of 128, one
+// token of 32 heads each (2.28 GB) 350 us, 6.5 TB/s. With 32 rows and 8-bit keys the matrix core
+// and the conversions have their share: 16 sequences of 501 to 16384 keys, 1 to 4 tokens of 64/8
+// heads (286 MB) 58 us and 5 the second kernel; with loads alone 2 less, so what is left is the start
+// (6 us until the first keys are there), and workgroups with the end of one sequence and the start of
+// another. One sequence of 777 keys 12 us: lengths, table, keys, join of the waves, ticket, join of
+// seven parts, a round trip each. What made it fast: the next step's loads in flight over a step's
+// products, always the same number of them so that the wait can tell them apart (89 -> 81 us);
+// sequences that count what changing to them costs (81 -> 69); table entries requested before rows
+// (69 -> 63). Tried and not kept: workgroups of their own for sequences of equal lengths (8 of 8192
+// keys, 8 tokens each, 60.5 -> 56.3 us, but 0.2 to 0.4 us more for every other call).
 #include "ef_device.hpp"
 #include "ef_serve.hpp"
 #include "group_combine.hpp"
@@ -31,12 +41,15 @@ namespace ef {
 namespace {
 
 constexpr int kUnit = 64;             // keys of a unit of work
-// Bytes of keys that a sequence counts beside its own: what a workgroup takes from one sequence to the
-// next (rows, table, the first loads' way, the join of its waves).
+// Bytes of keys that a sequence counts beside its own: what a workgroup takes from one sequence to
+// the next (rows, table, the first loads' way, the join of its waves). 31 sequences of 1122 keys of
+// 4 heads, e4m3, 64 / 128 / 192 / 256 KiB 16.7 / 17.5 / 18.6 / 20.5 us; 41 of 5098 of 8 heads 98.5 /
+// 99.8 / 98.6 / 97.0; 32 long ones 350 / 352 / 353 / 354.
 constexpr int kExtraBytes = 64 * 1024;
-constexpr int kWideChannels = 32;     // of a row that a workgroup joins from hundreds of parts
-constexpr float kHeadroom = 8.f;      // base-2 headroom before the reference moves
-constexpr int kStageBytes = 8192;     // keys, and values, of a wave's step
+constexpr int kWideChannels = 32;  // of a row that a workgroup joins from hundreds of parts
+constexpr float kHeadroom = 8.f;   // base-2 headroom before the reference moves
+constexpr int kStageBytes = 8192;  // keys, and values, of a wave's step
+
 // A value that is the same in all lanes, for the compiler to see.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 // Waits until at most N of the wave's loads are on their way.
@@ -350,12 +363,10 @@ __device__ __forceinline__ void attend_pages(const PagedParams& a) {
           const int page = __shfl(pv, (key >> a.c.shift) - p0, 64);
           const size_t cell = (((size_t)(unsigned)page * a.Hkv + hk) << a.c.shift) +
                               (unsigned)(key & page_mask);
-          __builtin_amdgcn_global_load_lds(a.c.k_scale + cell,
-                                           EF_LDS(void, (S == 0 ? sks0 : sks1)[wave] + 64 * x), 4, 0,
-                                           0);
-          __builtin_amdgcn_global_load_lds(a.c.v_scale + cell,
-                                           EF_LDS(void, (S == 0 ? svs0 : svs1)[wave] + 64 * x), 4, 0,
-                                           0);
+          float* const ks = (S == 0 ? sks0 : sks1)[wave] + 64 * x;
+          float* const vsc = (S == 0 ? svs0 : svs1)[wave] + 64 * x;
+          __builtin_amdgcn_global_load_lds(a.c.k_scale + cell, EF_LDS(void, ks), 4, 0, 0);
+          __builtin_amdgcn_global_load_lds(a.c.v_scale + cell, EF_LDS(void, vsc), 4, 0, 0);
         }
       }
     };

@@ -4,7 +4,9 @@
 // their row's scale. A workgroup takes up to 16 packed rows (tokens) of all heads; their sequences
 // and pages are found once and kept in LDS. A lane requests four pieces before it stores one.
 //
-// Bound by HBM: codes and rows read once, rows written once.
+// Bound by HBM: codes and rows read once, rows written once: 179000 positions of 8 heads of 128 in
+// bf16 (1.47 GB) 258 us, 5.7 TB/s (one piece at a time 276); 14 contexts of 264 of 32 heads of 64
+// 29 -> 13.6 us with the pieces in flight and fewer tokens to a workgroup.
 #include "ef_device.hpp"
 #include "ef_serve.hpp"
 

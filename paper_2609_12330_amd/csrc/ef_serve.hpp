@@ -79,6 +79,7 @@ struct PackedParams {
   const int* starts;
   const int* k_starts;
   uint16_t* o;
+  int* split;     // states of a kv head that the call makes
   float* ws_m;    // [Hkv][slots][128]
   float* ws_l;
   float* ws_acc;  // [Hkv][slots][128][D]

@@ -12,8 +12,10 @@
 // 8-bit rows: the largest magnitude of a row is taken over its D / 16 lanes; the scale is a power
 // of two, so x / s is exact and a code carries one rounding.
 //
-// Bound by HBM (each row read and written once), and for few tokens by latency: starts, then
-// lengths, then the table's entry, with the rows' loads beside them.
+// Bound by HBM (each row read and written once): 11006 tokens of 32 heads of 128 rotated (180 MB)
+// 32.7 us, 5.5 TB/s; prompts of 9000 tokens of 32/8 heads of 128 to an 8-bit cache (203 MB) 43 us, 4.7
+// TB/s, with the codes' arithmetic. For few tokens by latency: starts, then lengths, then the table's
+// entry, with the rows' loads beside them (one token of 16 sequences 3.9 us).
 #include "ef_device.hpp"
 #include "ef_serve.hpp"
 

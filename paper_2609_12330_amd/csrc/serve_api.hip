@@ -33,7 +33,7 @@ bool uneven(const int* starts, int T, int B) { return starts == nullptr && T % B
 ef_status check_pages(int pages, int page, int width, int format) {
   if (pages < 1 || width < 0 || (format != EF_CACHE_BF16 && format != EF_CACHE_E4M3) ||
       (page != 16 && page != 32 && page != 64 && page != 128 && page != 256) ||
-      (long long)width * page >= (1LL << 31))
+      (long long)width * page >= (1LL << 31) - 4096)  // (steps past the end count on)
     return EF_ERR_INVALID_PAGES;
   return EF_OK;
 }
@@ -130,11 +130,16 @@ ef_status paged_plan(PagedPlan& p, int T, int B, int Hq, int Hkv, int D, int max
 }
 
 // Launch shape of attention of packed sequences: see PackedParams. Row tiles of a kv head are at
-// most G T / 128 + B, and their keys are cut into parts of at least kLeastTiles tiles.
-constexpr int kLeastTiles = 8;
+// most G T / 128 + B, and their keys are cut into parts of at least `least` tiles: 128 rows' states
+// cost as much as ten tiles, with the second launch that joins them, those of a few rows little
+// more than that launch. At least 4 / 8 / 16 tiles: one prompt of 777 tokens of 32/8 heads of 128
+// [13 tiles] 41.9 / 41.7 / 19.2 us, one of 512 [8] 30.7 / 14.9 / 15.0; one token of 16 sequences of
+// 4 heads over 90 to 2311 keys 15.3 / 16.9 / 23.3, 19 to 44 of 9 of 16/4 heads over 2747 to 7262 39.3
+// / 40.8 / 47.0.
+constexpr int kLeastFull = 16, kLeastFew = 4, kFewRows = 64;
 
 struct PackedPlan {
-  int fill, slots, per_head;
+  int fill, least, slots, per_head;
   size_t m_off, l_off, acc_off, bytes;
 };
 
@@ -148,18 +153,19 @@ ef_status packed_plan(PackedPlan& p, int T, int Tk, int B, int Hq, int Hkv, int 
   const long long tiles = std::min(T * G / kRows + B, (long long)T * ((G + kRows - 1) / kRows));
   p.fill = std::max(kFillWgs / Hkv, 1);
   const long long key_tiles = ((long long)Tk + 63) / 64;
-  const long long parts = (key_tiles + kLeastTiles - 1) / kLeastTiles;
+  p.least = (long long)T * G >= (long long)kFewRows * B ? kLeastFull : kLeastFew;
+  const long long parts = (key_tiles + p.least - 1) / p.least;
   // A sequence of m row tiles and t > C key tiles has m ceil(t / C) < 2 m t / C units, and the
   // sum of m t over C is at most `fill`.
   p.slots = parts <= 1 ? 0 : (int)std::min<long long>(2LL * p.fill, tiles * parts);
   const long long per_head = tiles + p.slots;
-  if (per_head * Hkv > kMaxGroups) return EF_ERR_INVALID_SHAPE;
+  if (per_head * Hkv > kMaxGroups || 4LL * p.slots * Hkv > kMaxGroups) return EF_ERR_INVALID_SHAPE;
   p.per_head = (int)per_head;
   const size_t states = (size_t)Hkv * p.slots * kRows;
-  p.m_off = 0;
-  p.l_off = ef::ws_align256(states * sizeof(float));
-  p.acc_off = 2 * p.l_off;
-  p.bytes = p.acc_off + states * D * sizeof(float);
+  p.m_off = 256;  // behind their number
+  p.l_off = p.m_off + ef::ws_align256(states * sizeof(float));
+  p.acc_off = p.l_off + ef::ws_align256(states * sizeof(float));
+  p.bytes = p.slots == 0 ? 0 : p.acc_off + states * D * sizeof(float);
   return EF_OK;
 }
 
@@ -344,6 +350,7 @@ ef_status ef_attention_packed(const void* q, const void* k, const void* v, const
     if (workspace == nullptr || workspace_bytes < p.bytes) return EF_ERR_WORKSPACE_TOO_SMALL;
     if (misaligned(workspace)) return EF_ERR_MISALIGNED;
     char* const ws = static_cast<char*>(workspace);
+    a.split = reinterpret_cast<int*>(ws);
     a.ws_m = reinterpret_cast<float*>(ws + p.m_off);
     a.ws_l = reinterpret_cast<float*>(ws + p.l_off);
     a.ws_acc = reinterpret_cast<float*>(ws + p.acc_off);
@@ -358,7 +365,7 @@ ef_status ef_attention_packed(const void* q, const void* k, const void* v, const
   a.G = Hq / Hkv;
   a.causal = causal ? 1 : 0;
   a.fill = p.fill;
-  a.least = kLeastTiles;
+  a.least = p.least;
   a.slots = p.slots;
   a.per_head = p.per_head;
   a.c_abs = std::fabs(scale) * ef::kLog2e;

@@ -1302,7 +1302,8 @@ def attention_packed(q, k, v, starts, k_starts=None, causal: bool = True,
                                             (T, Tk, B, Hq, H, D), q, stream)
     st = _call_on(q, stream, _lib().ef_attention_packed, q.data_ptr(), k.data_ptr(), v.data_ptr(),
                   starts.data_ptr(), ks.data_ptr(), o.data_ptr(), T, Tk, B, Hq, H, D,
-                  1.0 / math.sqrt(D) if scale is None else float(scale), 1 if causal else 0, ptr, nbytes)
+                  1.0 / math.sqrt(D) if scale is None else float(scale), 1 if causal else 0, ptr,
+                  nbytes)
     if st:
         _check(st, "ef_attention_packed")
     return o

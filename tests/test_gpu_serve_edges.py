@@ -93,7 +93,8 @@ def test_empty_calls(Hq, H):
     p = Pages(11, H, 16, 64, [5], False)
     q = normal(12, 2, Hq, 64).cuda()
     none, empty = ints([]), torch.empty(0, Hq, 64, dtype=torch.bfloat16, device="cuda")
-    assert ef.attention_paged(empty, p.cache, p.dev_table[:0].contiguous(), none).shape == empty.shape
+    no_table = p.dev_table[:0].contiguous()
+    assert ef.attention_paged(empty, p.cache, no_table, none).shape == empty.shape
     assert ef.attention_packed(empty, empty, empty, ints([0])).shape == empty.shape
     wide = torch.empty(2, 0, dtype=torch.int32, device="cuda")  # tables without pages
     assert (ef.attention_paged(q, p.cache, wide, ints([9, 0])) == 0).all()
@@ -346,7 +347,8 @@ def test_counter_that_was_not_zero(Hq, H, counts):
     got = ef.attention_paged(q, p.cache, p.dev_table, ints([3000]), workspace=ws)
     assert torch.isnan(got).all() if counts else torch.equal(got, want)
     ef.workspace_counters(ws)[:] = 0
-    assert torch.equal(ef.attention_paged(q, p.cache, p.dev_table, ints([3000]), workspace=ws), want)
+    got = ef.attention_paged(q, p.cache, p.dev_table, ints([3000]), workspace=ws)
+    assert torch.equal(got, want)
 
 
 def test_refusals_of_the_binding():
