@@ -23,7 +23,7 @@
 // What bounds it: HBM where there is work: 32 sequences of 2001 to 32768 keys of 8 heads of 128, one
 // token of 32 heads each (2.28 GB) 350 us, 6.5 TB/s. With 32 rows and 8-bit keys the matrix core
 // and the conversions have their share: 16 sequences of 501 to 16384 keys, 1 to 4 tokens of 64/8
-// heads (286 MB) 58 us and 5 the second kernel; with loads alone 2 less, so what is left is the start
+// heads (286 MB) 58 us and 5 the second kernel; with loads alone 4 less, so what is left is the start
 // (6 us until the first keys are there), and workgroups with the end of one sequence and the start of
 // another. One sequence of 777 keys 12 us: lengths, table, keys, join of the waves, ticket, join of
 // seven parts, a round trip each. What made it fast: the next step's loads in flight over a step's
@@ -245,7 +245,8 @@ __device__ __forceinline__ void attend_pages(const PagedParams& a) {
     const int n = __builtin_amdgcn_readlane(s.n, at);
     const int start = __builtin_amdgcn_readlane(s.start, at);
     const int nrows = min(ROWS, min(n, a.max_queries) * a.G - row0);
-    const int end_seen = (row0 + nrows - 1) / a.G + len - n + 1;  // keys any row sees
+    const int end_seen =  // keys any row sees
+        (int)((unsigned)(row0 + nrows - 1) / (unsigned)a.G) + len - n + 1;
     const int k0 = uniform((u - first) * kUnit);
     const int u_next = min(u_end, first + units);
     const int k1 = min((u_next - first) * kUnit, end_seen);

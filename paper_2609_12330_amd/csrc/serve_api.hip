@@ -94,8 +94,13 @@ struct PagedPlan {
 
 constexpr int kMostWgs = 2048;
 static_assert(kMostWgs * 64 <= ef::kCounterRegionBytes, "a counter for every workgroup");
+// The last of a row's parts joins them in the same launch where rows are few (two of 128 to a wave)
+// and their parts not hundreds, or up to 16 rows where the table bounds the parts to a handful, that
+// is where mostly nothing is cut at all; a second launch otherwise, which costs 4 us and the
+// host 2 (one sequence of 166 keys of 8/2 heads of 128, second launch / same 11.1 / 8.4 us).
 constexpr int kJoinElems = 1024;
 constexpr int kJoinParts = 128;
+constexpr int kFewParts = 4;
 constexpr int kLeastKeys = 128;  // keys of a part, at least
 
 // `positions`: the table's, which bound the parts of a row (0 for the workspace's size, which does
@@ -115,9 +120,9 @@ ef_status paged_plan(PagedPlan& p, int T, int B, int Hq, int Hkv, int D, int max
   if (p.heads == 0) return EF_OK;
   p.W = std::max(1, std::max(kFillWgs / p.heads, std::min(B, kMostWgs / p.heads)));
   if ((long long)p.heads * p.W > kMaxGroups) return EF_ERR_INVALID_SHAPE;
-  // The last of a row's parts joins them in the same launch where these are few (see below).
   const long long parts = std::min<long long>(p.W, positions / kLeastKeys + 2);
-  p.fused = rows * D <= kJoinElems && parts <= kJoinParts && p.heads * p.W <= kMostWgs;
+  p.fused = p.rt == 1 && p.heads * p.W <= kMostWgs &&
+            ((rows * D <= kJoinElems && parts <= kJoinParts) || parts <= kFewParts);
   if (!p.fused && (long long)B * p.heads * std::min(rows, tile) * 4 > kMaxGroups)
     return EF_ERR_INVALID_SHAPE;
   const size_t states = (size_t)p.heads * p.W * 2 * tile;
