@@ -375,6 +375,7 @@ __device__ __forceinline__ void attend_pages(const PagedParams& a) {
     // the compiler was seen to leave out the wait for one of the stages in LDS.)
     constexpr int LOADS = 16 + (E4M3 ? 2 * (KT / 64) : 0);  // of a step
     auto landed = [] {
+      asm volatile("" ::: "memory");  // (no load of the next step sinks below the wait)
       __builtin_amdgcn_sched_barrier(0);
       wait_loads<LOADS>();
       __builtin_amdgcn_sched_barrier(0);
