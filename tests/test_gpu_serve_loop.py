@@ -124,3 +124,58 @@ def test_serving_loop(Hq, H, D, page, e4m3):
         again = ef.attention_paged(turned, s.cache, s.dev_table, dev_lengths, workspace=ws)
         assert torch.equal(again, out), i
     assert not ef.workspace_counters(ws).any()
+
+
+@pytest.mark.parametrize("Hq,H,D,e4m3", [(8, 1, 128, False), (8, 2, 64, True)])
+def test_chunk_as_a_graph(Hq, H, D, e4m3):
+    """A chunk of every sequence, written, read back and attended (with keys cut into parts), captured
+    once and replayed with other tokens, lengths and starts, eager work between."""
+    announce(f"chunk graph {Hq} {H} {D} {e4m3}")
+    room = [5000, 3000, 300]
+    s = Loop(Hq, H, D, 32, e4m3, room, seed=140)
+    T, Tk = 96, sum(room)
+    q, k, v = s.tokens(T)
+    lengths, starts, ks = ints([0] * 3), ints([0] * 4), ints([0] * 4)
+    kr, vr = (torch.zeros(Tk, H, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    turned, out = torch.empty_like(q), torch.empty_like(q)
+    ws = ef.make_packed_workspace(q, kr, 3)
+    assert ws is not None
+
+    def chunk():
+        ef.cache_write(s.cache, k, v, s.dev_table, lengths, starts=starts, q=q, rope=s.rope,
+                       q_out=turned)
+        ef.cache_read(s.cache, s.dev_table, ks, k_out=kr, v_out=vr)
+        ef.attention_packed(turned, kr, vr, starts, ks, workspace=ws, out=out)
+
+    def at(new, keys):
+        for t, values in ((lengths, keys), (starts, starts_of(new)), (ks, starts_of(keys))):
+            t.copy_(torch.tensor(values, dtype=torch.int32))
+        for x, y in zip((q, k, v), s.tokens(T)):
+            x.copy_(y)
+
+    at([0, 0, 0], [0, 0, 0])
+    chunk()  # (no row at all)
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            chunk()
+    torch.cuda.synchronize()
+    # Caches of zeros: what a chunk attends to before all of it was written is well defined.
+    for t in (s.cache.k, s.cache.v):
+        t.view(torch.uint8).zero_()
+    if e4m3:
+        s.cache.k_scale.fill_(1.0)
+        s.cache.v_scale.fill_(1.0)
+    for i, (new, keys) in enumerate((([64, 32, 0], [4000, 32, 0]), ([1, 90, 5], [4001, 3000, 5]),
+                                     ([90, 0, 6], [5000, 3000, 11]), ([3, 3, 3], [7, 2000, 300]))):
+        at(new, keys)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        n = sum(new)
+        s.check(got[:n], turned[:n], starts_of(new), keys, f"replay {i}")
+        chunk()
+        torch.cuda.synchronize()
+        assert torch.equal(out[:n], got[:n]), i
