@@ -145,7 +145,7 @@ constexpr int kLeastFull = 16, kLeastFew = 4, kFewRows = 64;
 
 struct PackedPlan {
   int fill, least, slots, per_head;
-  size_t m_off, l_off, acc_off, bytes;
+  size_t split_off, m_off, l_off, acc_off, bytes;
 };
 
 ef_status packed_plan(PackedPlan& p, int T, int Tk, int B, int Hq, int Hkv, int D) {
@@ -167,7 +167,9 @@ ef_status packed_plan(PackedPlan& p, int T, int Tk, int B, int Hq, int Hkv, int 
   if (per_head * Hkv > kMaxGroups || 4LL * p.slots * Hkv > kMaxGroups) return EF_ERR_INVALID_SHAPE;
   p.per_head = (int)per_head;
   const size_t states = (size_t)Hkv * p.slots * kRows;
-  p.m_off = 256;  // behind their number
+  // The counters that other calls keep at the start of a workspace are left alone.
+  p.split_off = ef::kCounterRegionBytes;
+  p.m_off = p.split_off + 256;
   p.l_off = p.m_off + ef::ws_align256(states * sizeof(float));
   p.acc_off = p.l_off + ef::ws_align256(states * sizeof(float));
   p.bytes = p.slots == 0 ? 0 : p.acc_off + states * D * sizeof(float);
@@ -355,7 +357,7 @@ ef_status ef_attention_packed(const void* q, const void* k, const void* v, const
     if (workspace == nullptr || workspace_bytes < p.bytes) return EF_ERR_WORKSPACE_TOO_SMALL;
     if (misaligned(workspace)) return EF_ERR_MISALIGNED;
     char* const ws = static_cast<char*>(workspace);
-    a.split = reinterpret_cast<int*>(ws);
+    a.split = reinterpret_cast<int*>(ws + p.split_off);
     a.ws_m = reinterpret_cast<float*>(ws + p.m_off);
     a.ws_l = reinterpret_cast<float*>(ws + p.l_off);
     a.ws_acc = reinterpret_cast<float*>(ws + p.acc_off);

@@ -334,6 +334,27 @@ def test_streams_and_workspaces():
         torch.cuda.synchronize()
 
 
+def test_workspace_of_several_operators():
+    """Attention of packed sequences leaves the counters of a shared workspace alone."""
+    announce("a workspace for both")
+    p = Pages(49, 2, 16, 128, [1500, 700], False)
+    q = normal(50, 2, 8, 128).cuda()
+    starts, ks = [0, 5, 9], [0, 4000, 9000]
+    qp = normal(51, 9, 8, 128).cuda()
+    k, v = normal(52, 9000, 2, 128).cuda(), normal(53, 9000, 2, 128).cuda()
+    alone = (ef.attention_paged(q, p.cache, p.dev_table, ints([1500, 700])),
+             ef.attention_packed(qp, k, v, ints(starts), ints(ks)))
+    n = max(ef.ef_attention_paged_workspace_size(2, 2, 8, 2, 128, 1),
+            ef.ef_attention_packed_workspace_size(9, 9000, 2, 8, 2, 128))
+    ws = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    for _ in range(3):
+        got = ef.attention_packed(qp, k, v, ints(starts), ints(ks), workspace=ws)
+        assert torch.equal(got, alone[1])
+        assert not ws[:ef.COUNTER_REGION_BYTES].any()
+        got = ef.attention_paged(q, p.cache, p.dev_table, ints([1500, 700]), workspace=ws)
+        assert torch.equal(got, alone[0])
+
+
 @pytest.mark.parametrize("Hq,H,counts", [(8, 2, True), (16, 8, True), (32, 2, False)])
 def test_counter_that_was_not_zero(Hq, H, counts):
     """From the number of parts on: NaN rows, and the region cleared makes it good again. (The parts

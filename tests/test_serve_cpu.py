@@ -129,7 +129,7 @@ def test_workspace_sizes():
         assert size(n * 8, n, 64, 8, 128, 8) >= size(n, n, 64, 8, 128, 1)
     size = ef.ef_attention_packed_workspace_size
     assert size(100, 500, 3, 32, 8, 128) == 0           # too few keys to cut
-    assert size(100, 50000, 3, 32, 8, 128) > 0
+    assert size(100, 50000, 3, 32, 8, 128) > ef.COUNTER_REGION_BYTES
     assert size(0, 50000, 3, 32, 8, 128) == size(100, 50000, 3, 31, 8, 128) == 0
 
 
