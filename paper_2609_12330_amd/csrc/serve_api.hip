@@ -21,8 +21,8 @@ ef_status check_heads(int T, int B, int Hq, int Hkv, int D) {
   if (T < 0 || B < 0 || Hq < 1 || Hkv < 1) return EF_ERR_INVALID_SHAPE;
   if (Hq % Hkv != 0) return EF_ERR_GQA_RATIO;
   if (D != 64 && D != 128) return EF_ERR_UNSUPPORTED_HEAD_DIM;
-  // Rows of a kv head and byte offsets inside a 64-row tile stay below 2^31.
-  if (Hkv > kMaxGridYZ || B > (1 << 30) || (long long)T * (Hq / Hkv) >= (1LL << 31) - 128)
+  // Rows of a token or a kv head and byte offsets inside a 64-row tile stay below 2^31.
+  if (Hkv > kMaxGridYZ || Hq > (1 << 30) || B > (1 << 30) || (long long)T * (Hq / Hkv) >= (1LL << 31) - 128)
     return EF_ERR_INVALID_SHAPE;
   return EF_OK;
 }

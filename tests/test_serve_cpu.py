@@ -76,6 +76,7 @@ REFUSED = [
     (write, dict(B=-1), SHAPE), (write, dict(starts=None, T=7), SHAPE), (write, dict(k=MIS), MISAL),
     (write, dict(q=MIS), MISAL), (write, dict(k_cache=MIS), MISAL), (write, dict(table=MIS4), MISAL),
     (write, dict(lengths=MIS4), MISAL), (write, dict(starts=MIS4), MISAL),
+    (write, dict(T=3, Hq=65535 * 32767, Hkv=65535), SHAPE),  # more rows of a token than are counted
     (read, dict(k_cache=None), NULL), (read, dict(starts=None), NULL), (read, dict(k_out=None), NULL),
     (read, dict(v_out=None), NULL), (read, dict(table=None), NULL), (read, dict(format=1), NULL),
     (read, dict(page=20), PAGES), (read, dict(pages=-1), PAGES), (read, dict(D=100), DIM),
