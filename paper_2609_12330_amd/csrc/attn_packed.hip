@@ -149,8 +149,10 @@ __device__ __forceinline__ int most_tiles(const PackedParams& a, Cut& c, int& ro
   }
   if (a.slots == 0) return 0x7fffffff;
   const int places = rows >= a.fill ? a.fill : max(a.fill - rows, (a.fill + 1) / 2);
-  // At least work / places, for all that fp32 rounds: the states' room counts on it.
-  const int most = (int)fminf(work * 1.001f / (float)places + 1.f, 2e9f);
+  // At least work / places, for all that fp32 rounds (half a step for each 64 sequences, 1e-9 of
+  // the sum for one): the states' room counts on it.
+  const float room = 1.001f + 1e-9f * (float)a.B;
+  const int most = (int)fminf(work * room / (float)places + 1.f, 2e9f);
   return max(__builtin_amdgcn_readfirstlane(most), a.least);
 }
 
