@@ -953,7 +953,9 @@ def rope_turns(rot: int, base: float = 10000.0, scaling: str = "none", factor: f
                 factor, the fastest stays;
       "turns"   pairs that turn `high` times or more in `length` positions stay, those that turn
                 `low` times or fewer are divided by factor, between them linear in their turns;
-      "index"   the same borders, between them linear in the pair's number."""
+      "index"   the same borders as numbers of pairs, rounded outwards to whole ones in 0 .. rot - 1
+                (the one of `low` may lie behind the last pair), between them linear in the
+                pair's number."""
     torch = _torch()
     if rot < 2 or rot % 2:
         raise ValueError("rot must be a positive even number")
@@ -980,7 +982,7 @@ def rope_turns(rot: int, base: float = 10000.0, scaling: str = "none", factor: f
 
         def at(turns):  # number of the pair that turns so often in `length`
             return rot * math.log(length / (turns * 2 * math.pi)) / (2 * math.log(base))
-        first, last = max(math.floor(at(high)), 0), min(math.ceil(at(low)), rot // 2 - 1)
+        first, last = max(math.floor(at(high)), 0), min(math.ceil(at(low)), rot - 1)
         keep = 1 - ((i - first) / max(last - first, 0.001)).clamp(0, 1)
         return t * keep + t / factor * (1 - keep)
     return t
