@@ -977,8 +977,8 @@ def rope_turns(rot: int, base: float = 10000.0, scaling: str = "none", factor: f
         keep = ((length * t - low) / (high - low)).clamp(0, 1)
         return t * keep + t / factor * (1 - keep)
     if scaling == "index":
-        if base == 1.0:
-            raise ValueError("scaling 'index' needs base != 1")
+        if base <= 1.0:  # (turns would not fall along the pairs)
+            raise ValueError("scaling 'index' needs base > 1")
 
         def at(turns):  # number of the pair that turns so often in `length`
             return rot * math.log(length / (turns * 2 * math.pi)) / (2 * math.log(base))

@@ -62,3 +62,12 @@ def test_index_scaling_of_the_last_pair():
                                             high=32.0)
     assert 1.6 < 32768 * t[-1] < 1.7
     assert math.isclose(s[-1] / t[-1], 0.25 + 0.75 / 8, rel_tol=1e-12)
+
+
+@pytest.mark.parametrize("base", [0.5, 0.999, 1.0])
+def test_index_scaling_needs_falling_turns(base):
+    """With a base below 1 later pairs turn more often and the borders change places."""
+    with pytest.raises(ValueError, match="base > 1"):
+        ef.rope_turns(16, base, scaling="index", factor=8.0, length=64, low=1.0, high=32.0)
+    assert ef.rope_turns(16, base, scaling="turns", factor=8.0, length=64, low=1.0,
+                         high=32.0).shape == (8,)
