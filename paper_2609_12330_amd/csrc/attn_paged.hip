@@ -31,6 +31,8 @@
 // sequences that count what changing to them costs (81 -> 69); table entries requested before rows
 // (69 -> 63). Tried and not kept: workgroups of their own for sequences of equal lengths (8 of 8192
 // keys, 8 tokens each, 60.5 -> 56.3 us, but 0.2 to 0.4 us more for every other call).
+#include <algorithm>
+
 #include "ef_device.hpp"
 #include "ef_serve.hpp"
 #include "group_combine.hpp"
@@ -706,15 +708,15 @@ void attn_paged_kernel(PagedParams a) {
 }
 
 // Joins the parts of a row that several workgroups share: a wave a row, or (WIDE) four waves for 32
-// channels of it, each a quarter of the parts.
+// channels of it, each a quarter of the parts. Sequences from b0 on.
 template <int D, int ROWS, bool WIDE>
-__global__ __launch_bounds__(256) void paged_combine_kernel(PagedParams a, int tiles) {
+__global__ __launch_bounds__(256) void paged_combine_kernel(PagedParams a, int tiles, int b0) {
   constexpr int CH = WIDE ? kWideChannels : D;  // channels of a wave
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int x = (int)(blockIdx.x % tiles);
   const int r = WIDE ? x / (D / CH) : x * 4 + wave, c0 = WIDE ? x % (D / CH) * CH : 0;
   const int head = (int)(blockIdx.x / tiles % a.heads);
-  const int b = (int)(blockIdx.x / tiles / a.heads);
+  const int b = b0 + (int)(blockIdx.x / tiles / a.heads);
   const int mt = head % a.mtiles, hk = head / a.mtiles;
   const int2 part = a.parts[(size_t)b * a.heads + head];
   const int start = sequence_start(a.starts, b, a.B, a.T);
@@ -761,20 +763,23 @@ hipError_t launch(const PagedParams& a, hipStream_t stream) {
   hipLaunchKernelGGL((attn_paged_kernel<D, E4M3, RT, NT>), dim3((unsigned)a.heads * a.W), dim3(256),
                      0, stream, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.counters != nullptr) return e;
+  // (One workgroup for all of a head's keys cuts nothing.)
+  if (e != hipSuccess || a.counters != nullptr || a.W == 1) return e;
   // A wave a row where the parts may be few; where there may be hundreds, four waves for every 32
   // channels of a row.
   const int rows = a.mtiles > 1 ? 16 * RT : a.rows;
   const bool wide = a.W > 128;
   const int tiles = wide ? rows * (D / kWideChannels) : (rows + 3) / 4;
-  const dim3 grid((unsigned)a.B * a.heads * tiles);
-  if (wide)
-    hipLaunchKernelGGL((paged_combine_kernel<D, 16 * RT, true>), grid, dim3(256), 0, stream, a,
-                       tiles);
-  else
-    hipLaunchKernelGGL((paged_combine_kernel<D, 16 * RT, false>), grid, dim3(256), 0, stream, a,
-                       tiles);
-  return hipGetLastError();
+  auto* const combine = wide ? paged_combine_kernel<D, 16 * RT, true>
+                             : paged_combine_kernel<D, 16 * RT, false>;
+  // Sequences of a launch. (W > 1 leaves at most 1024 heads of 8 tiles, or 16 of 128.)
+  const int most = (int)(kMaxGroups / ((long long)a.heads * tiles));
+  for (int b0 = 0; b0 < a.B && e == hipSuccess; b0 += most) {
+    const dim3 grid((unsigned)std::min(most, a.B - b0) * a.heads * tiles);
+    hipLaunchKernelGGL(combine, grid, dim3(256), 0, stream, a, tiles, b0);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 template <int D, bool E4M3>

@@ -7,6 +7,9 @@
 
 namespace ef {
 
+// Workgroups of a launch: it holds fewer than 2^32 threads, and these stay well below.
+constexpr long long kMaxGroups = (1LL << 31) / 256;
+
 // A cache in pages: k, v [pages][Hkv][page][D], bf16 or e4m3 codes with a scale a row.
 struct PagesParams {
   char* k;

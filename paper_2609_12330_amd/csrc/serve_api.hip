@@ -12,8 +12,7 @@ namespace {
 
 using namespace ef::host;
 
-// A launch holds fewer than 2^32 threads; these stay well below.
-constexpr long long kMaxGroups = (1LL << 31) / 256;
+using ef::kMaxGroups;
 
 bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 
@@ -123,8 +122,6 @@ ef_status paged_plan(PagedPlan& p, int T, int B, int Hq, int Hkv, int D, int max
   const long long parts = std::min<long long>(p.W, positions / kLeastKeys + 2);
   p.fused = p.rt == 1 && p.heads * p.W <= kMostWgs &&
             ((rows * D <= kJoinElems && parts <= kJoinParts) || parts <= kFewParts);
-  if (!p.fused && (long long)B * p.heads * std::min(rows, tile) * 4 > kMaxGroups)
-    return EF_ERR_INVALID_SHAPE;
   const size_t states = (size_t)p.heads * p.W * 2 * tile;
   p.parts_off = ef::kCounterRegionBytes;
   p.m_off = p.parts_off + ef::ws_align256((size_t)B * p.heads * sizeof(int2));

@@ -1,0 +1,31 @@
+"""Attention over pages where one sequence has a chunk of its prompt and many others a single token:
+launches without a second one, with one, and with several. Tolerance of long_helpers.py."""
+
+import pytest
+
+from long_helpers import _gpu, announce  # noqa: F401
+from test_gpu_serve_attention import run_paged
+
+pytestmark = pytest.mark.gpu
+
+
+def beside(chunk, keys, at, B):
+    """new tokens and lengths of B sequences, the one at `at` with a chunk."""
+    new, lengths = [1] * B, [1 + 37 * i % 400 for i in range(B)]
+    new[at], lengths[at] = chunk, keys
+    return new, lengths
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("Hq,H,D,page,chunk,keys,at,B", [
+    # 2048 heads and row tiles: a workgroup each, nothing is cut.
+    (64, 8, 64, 16, 1024, 1100, 0, 34),
+    # 1024: two each, which cut the chunk's keys.
+    (64, 8, 128, 64, 512, 3000, 33, 66),
+    # The parts of 1024 sequences are joined by a launch, those behind them by another.
+    (64, 8, 64, 32, 512, 1500, 1050, 1100),
+])
+def test_chunk_beside_many_sequences(Hq, H, D, page, chunk, keys, at, B, e4m3):
+    announce(f"chunk of {chunk} over {keys} at {at} of {B} e4m3 {e4m3}")
+    new, lengths = beside(chunk, keys, at, B)
+    run_paged((Hq, H, D, page, new, lengths), e4m3)
