@@ -628,7 +628,8 @@ ef_status ef_cache_read(const void* k_cache, const void* v_cache, const float* k
  *               max_queries rows are written. With starts = NULL at least T / B.
  *   workspace : ef_attention_paged_workspace_size(...) bytes, 16-byte aligned, with the
  *               counter region of ef_attention_splitkv's workspace at its start; the same rules.
- *               Its size does not depend on lengths.
+ *               Its size does not depend on lengths, and one for larger T, B and max_queries
+ *               serves smaller ones.
  * Limits beside those of the other calls: B (width page / 64 + 32) < 2^31 (units of work that are
  * counted in 32 bits), and max_queries Hq / 32 <= 2^23 (workgroups of a launch).
  * The keys of all sequences are dealt evenly to the compute units, whatever their lengths.

@@ -122,7 +122,12 @@ ef_status paged_plan(PagedPlan& p, int T, int B, int Hq, int Hkv, int D, int max
   const long long parts = std::min<long long>(p.W, positions / kLeastKeys + 2);
   p.fused = p.rt == 1 && p.heads * p.W <= kMostWgs &&
             ((rows * D <= kJoinElems && parts <= kJoinParts) || parts <= kFewParts);
-  const size_t states = (size_t)p.heads * p.W * 2 * tile;
+  // Two states a workgroup where keys are cut (W > 1), or as many as any smaller call has: a
+  // workspace for the largest one serves them all.
+  const long long most =
+      B == 1 ? kFillWgs
+             : std::max<long long>(kFillWgs, std::min<long long>((long long)B * p.heads, kMostWgs));
+  const size_t states = (size_t)most * 2 * tile;
   p.parts_off = ef::kCounterRegionBytes;
   p.m_off = p.parts_off + ef::ws_align256((size_t)B * p.heads * sizeof(int2));
   p.l_off = p.m_off + ef::ws_align256(states * sizeof(float));

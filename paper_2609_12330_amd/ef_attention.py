@@ -1205,8 +1205,8 @@ def cache_read(cache: PagedCache, table, starts, total: Optional[int] = None, k_
 
 def make_paged_workspace(q, cache: PagedCache, B: int, max_queries: int = 1, stream=None):
     """A workspace for attention_paged on queries shaped like q [T, Hq, D] of B sequences, whatever
-    their lengths. Its memory and the clearing of its counters belong to `stream`, or to the
-    current one: calls on another stream have to wait for that."""
+    their lengths, and for smaller T, B and max_queries. Its memory and the clearing of its counters
+    belong to `stream`, or to the current one: calls on another stream have to wait for that."""
     T, Hq, D = q.shape
     n = int(ef_attention_paged_workspace_size(T, B, Hq, cache.shape[1], D, max_queries))
     return _state_workspace(n, q, stream)

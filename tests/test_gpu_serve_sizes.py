@@ -2,8 +2,11 @@
 launches without a second one, with one, and with several. Tolerance of long_helpers.py."""
 
 import pytest
+import torch
 
-from long_helpers import _gpu, announce  # noqa: F401
+from long_helpers import _gpu, announce, normal  # noqa: F401
+from paper_2609_12330_amd import ef_attention as ef
+from serve_helpers import Pages, ints, starts_of
 from test_gpu_serve_attention import run_paged
 
 pytestmark = pytest.mark.gpu
@@ -29,3 +32,22 @@ def test_chunk_beside_many_sequences(Hq, H, D, page, chunk, keys, at, B, e4m3):
     announce(f"chunk of {chunk} over {keys} at {at} of {B} e4m3 {e4m3}")
     new, lengths = beside(chunk, keys, at, B)
     run_paged((Hq, H, D, page, new, lengths), e4m3)
+
+
+def test_paged_workspace_of_the_largest_call():
+    """One made for a chunk of 520 tokens serves all shorter ones, with the same results as their own."""
+    announce("a paged workspace for smaller calls")
+    B, lengths = 16, [530 + 60 * i for i in range(16)]
+    p = Pages(120, 8, 64, 64, lengths, False)
+    q = normal(121, 520 + B - 1, 64, 64).cuda()
+    ws = ef.make_paged_workspace(q, p.cache, B, 520)
+    for n in (520, 500, 257, 40, 4, 1):
+        new = [n] + [1] * (B - 1)
+        qn, starts = q[:sum(new)].contiguous(), ints(starts_of(new))
+        got = ef.attention_paged(qn, p.cache, p.dev_table, ints(lengths), starts=starts, max_queries=n,
+                                 workspace=ws)
+        own = ef.attention_paged(qn, p.cache, p.dev_table, ints(lengths), starts=starts, max_queries=n)
+        assert torch.isfinite(got).all() and torch.equal(got, own), n
+    few = ints(lengths[:3])
+    got = ef.attention_paged(q[:3], p.cache, p.dev_table[:3].contiguous(), few, workspace=ws)
+    assert torch.equal(got, ef.attention_paged(q[:3], p.cache, p.dev_table[:3].contiguous(), few))

@@ -1,6 +1,7 @@
 """Which sizes the serving entry points take, and how their workspaces grow. No call here reaches a GPU."""
 
 import os
+import random
 
 import pytest
 
@@ -38,3 +39,27 @@ def test_most_row_tiles():
     """max_queries Hq / 32 workgroups of a launch, up to 2^23."""
     assert paged_without_workspace(2 ** 23, 1, 32, 8, 128, 2 ** 23) == WS
     assert paged_without_workspace(2 ** 23 + 8, 1, 32, 8, 128, 2 ** 23 + 8) == SHAPE
+
+
+def spread(rng, most):
+    """A number up to `most`, over its logarithm."""
+    return max(1, round(most ** rng.random()))
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(32, 8, 128), (64, 8, 64), (12, 12, 64), (6, 3, 128), (16, 1, 128),
+                                      (2100, 700, 64), (3000, 3000, 64)])
+def test_paged_workspace_serves_smaller_calls(Hq, Hkv, D):
+    rng = random.Random(Hq)
+    for _ in range(4000):
+        T, B, n = spread(rng, 100000), spread(rng, 5000), spread(rng, 10000)
+        large = paged_size(T, B, Hq, Hkv, D, n)
+        assert large > 0
+        for smaller in ((spread(rng, T), spread(rng, B), spread(rng, n)), (T, B, spread(rng, n)),
+                        (T, B, max(n - 1, 1)), (max(T - 1, 1), B, n), (T, max(B - 1, 1), n)):
+            assert paged_size(*smaller[:2], Hq, Hkv, D, smaller[2]) <= large, (T, B, n, smaller)
+
+
+def test_paged_workspace_of_one_chunk():
+    """Each step of a growing chunk, where a head's workgroups go from two to one."""
+    sizes = [paged_size(8192, 16, 32, 8, 128, n) for n in range(1, 3000)]
+    assert sizes == sorted(sizes) and sizes[-1] < 2 ** 27
