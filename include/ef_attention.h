@@ -655,9 +655,10 @@ size_t ef_attention_paged_workspace_size(int T, int B, int Hq, int Hkv, int D, i
  *   starts   : [B + 1] int32, the sequences' rows of q.
  *   k_starts : [B + 1] int32, their rows of k and v.
  *   workspace : ef_attention_packed_workspace_size(...) bytes, 16-byte aligned (may be NULL where
- *              that is 0). It holds partial states where few rows have many keys, behind the
- *              counter region of ef_attention_splitkv's workspace, which is not touched: one
- *              workspace serves both. Calls that overlap in time must not share one.
+ *              that is 0); one for larger T, Tk and B serves smaller ones. It holds partial states
+ *              where few rows have many keys, behind the counter region of ef_attention_splitkv's
+ *              workspace, which is not touched: one workspace serves both. Calls that overlap in
+ *              time must not share one.
  */
 ef_status ef_attention_packed(const void* q, const void* k, const void* v, const int* starts,
                               const int* k_starts, void* o, int T, int Tk, int B, int Hq, int Hkv,

@@ -144,11 +144,27 @@ ef_status paged_plan(PagedPlan& p, int T, int B, int Hq, int Hkv, int D, int max
 // 4 heads over 90 to 2311 keys 15.3 / 16.9 / 23.3, 19 to 44 of 9 of 16/4 heads over 2747 to 7262 39.3
 // / 40.8 / 47.0.
 constexpr int kLeastFull = 16, kLeastFew = 4, kFewRows = 64;
+// Key tiles of a call that are not cut, whatever the rows: the second launch costs more than two parts
+// save (one token over 320 keys of 32/8 heads of 128, cut / whole 11.1 / 9.1 us, over 512 11.9 / 11.7,
+// of 64/8 heads of 64 10.8 / 9.3; over 777 12.2 / 16.0).
+constexpr int kWholeTiles = 8;
 
 struct PackedPlan {
   int fill, least, slots, per_head;
-  size_t split_off, m_off, l_off, acc_off, bytes;
+  size_t split_off, m_off, l_off, acc_off;
+  size_t need, bytes;  // of this call, and of one of as many or more rows, keys and sequences
 };
+
+// Bytes of a workspace with `slots` states of a kv head.
+size_t packed_layout(PackedPlan& p, int slots, int Hkv, int D) {
+  const size_t states = (size_t)Hkv * slots * 128;
+  // The counters that other calls keep at the start of a workspace are left alone.
+  p.split_off = ef::kCounterRegionBytes;
+  p.m_off = p.split_off + 256;
+  p.l_off = p.m_off + ef::ws_align256(states * sizeof(float));
+  p.acc_off = p.l_off + ef::ws_align256(states * sizeof(float));
+  return slots == 0 ? 0 : p.acc_off + states * D * sizeof(float);
+}
 
 ef_status packed_plan(PackedPlan& p, int T, int Tk, int B, int Hq, int Hkv, int D) {
   const ef_status st = check_heads(T, B, Hq, Hkv, D);
@@ -161,20 +177,22 @@ ef_status packed_plan(PackedPlan& p, int T, int Tk, int B, int Hq, int Hkv, int 
   p.fill = std::max(kFillWgs / Hkv, 1);
   const long long key_tiles = ((long long)Tk + 63) / 64;
   p.least = (long long)T * G >= (long long)kFewRows * B ? kLeastFull : kLeastFew;
-  const long long parts = (key_tiles + p.least - 1) / p.least;
   // A sequence of m row tiles and t > C key tiles has m ceil(t / C) < 2 m t / C units, and the
   // sum of m t over C is at most `fill`.
-  p.slots = parts <= 1 ? 0 : (int)std::min<long long>(2LL * p.fill, tiles * parts);
+  auto states = [&](int least) {
+    const long long parts = (key_tiles + least - 1) / least;
+    return key_tiles <= kWholeTiles || parts <= 1
+               ? 0
+               : (int)std::min<long long>(2LL * p.fill, tiles * parts);
+  };
+  // (More rows may be cut less, so a workspace has room for the shortest parts: one for the largest
+  // call serves all smaller ones.)
+  p.bytes = packed_layout(p, states(kLeastFew), Hkv, D);
+  p.slots = states(p.least);
   const long long per_head = tiles + p.slots;
   if (per_head * Hkv > kMaxGroups || 4LL * p.slots * Hkv > kMaxGroups) return EF_ERR_INVALID_SHAPE;
   p.per_head = (int)per_head;
-  const size_t states = (size_t)Hkv * p.slots * kRows;
-  // The counters that other calls keep at the start of a workspace are left alone.
-  p.split_off = ef::kCounterRegionBytes;
-  p.m_off = p.split_off + 256;
-  p.l_off = p.m_off + ef::ws_align256(states * sizeof(float));
-  p.acc_off = p.l_off + ef::ws_align256(states * sizeof(float));
-  p.bytes = p.slots == 0 ? 0 : p.acc_off + states * D * sizeof(float);
+  p.need = packed_layout(p, p.slots, Hkv, D);
   return EF_OK;
 }
 
@@ -356,7 +374,7 @@ ef_status ef_attention_packed(const void* q, const void* k, const void* v, const
     return EF_ERR_MISALIGNED;
   ef::PackedParams a{};
   if (p.slots > 0) {
-    if (workspace == nullptr || workspace_bytes < p.bytes) return EF_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace == nullptr || workspace_bytes < p.need) return EF_ERR_WORKSPACE_TOO_SMALL;
     if (misaligned(workspace)) return EF_ERR_MISALIGNED;
     char* const ws = static_cast<char*>(workspace);
     a.split = reinterpret_cast<int*>(ws + p.split_off);

@@ -842,13 +842,15 @@ def _state_workspace(n, q, stream=None):
     return None if n == 0 else _zeros(n, q, stream, COUNTER_REGION_BYTES)
 
 
-def _own_workspace(workspace, size, sizes, q, stream):
-    """(pointer, bytes, tensor) of the workspace given, or of a new one of size(*sizes) bytes."""
+def _own_workspace(workspace, size, sizes, q, stream, counters=True):
+    """(pointer, bytes, tensor) of the workspace given, or of a new one of size(*sizes) bytes, its
+    counters cleared where the call has any."""
     if workspace is None:
         n = size(*sizes)
         if n == 0:
             return None, 0, None
-        workspace = _state_workspace(n, q, stream)
+        workspace = (_state_workspace(n, q, stream) if counters else
+                     _new((n,), _torch().uint8, q, stream))
     if workspace.get_device() != q.get_device() or not workspace.is_contiguous():
         _check_workspace(workspace, q)
     return workspace.data_ptr(), workspace.nbytes, workspace
@@ -1259,8 +1261,9 @@ def attention_paged(q, cache: PagedCache, table, lengths, starts=None,
 
 
 def make_packed_workspace(q, k, B: int, stream=None):
-    """A workspace for attention_packed on q [T, Hq, D] and k [Tk, Hkv, D] of B sequences (None
-    where none is needed). Its memory belongs to a stream as make_paged_workspace's does."""
+    """A workspace for attention_packed on q [T, Hq, D] and k [Tk, Hkv, D] of B sequences, and for
+    smaller T, Tk and B (None where none of them needs one). Its memory belongs to a stream as
+    make_paged_workspace's does."""
     n = int(ef_attention_packed_workspace_size(q.shape[0], k.shape[0], B, q.shape[1], k.shape[1],
                                                q.shape[2]))
     return _state_workspace(n, q, stream)
@@ -1301,7 +1304,7 @@ def attention_packed(q, k, v, starts, k_starts=None, causal: bool = True,
     if out is None:
         o = _new(q.shape, bf16, q, stream)
     ptr, nbytes, workspace = _own_workspace(workspace, ef_attention_packed_workspace_size,
-                                            (T, Tk, B, Hq, H, D), q, stream)
+                                            (T, Tk, B, Hq, H, D), q, stream, counters=False)
     st = _call_on(q, stream, _lib().ef_attention_packed, q.data_ptr(), k.data_ptr(), v.data_ptr(),
                   starts.data_ptr(), ks.data_ptr(), o.data_ptr(), T, Tk, B, Hq, H, D,
                   1.0 / math.sqrt(D) if scale is None else float(scale), 1 if causal else 0, ptr,

@@ -7,7 +7,7 @@ import torch
 from long_helpers import _gpu, announce, normal  # noqa: F401
 from paper_2609_12330_amd import ef_attention as ef
 from serve_helpers import Pages, ints, starts_of
-from test_gpu_serve_attention import run_paged
+from test_gpu_serve_attention import run_packed, run_paged
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +51,19 @@ def test_paged_workspace_of_the_largest_call():
     few = ints(lengths[:3])
     got = ef.attention_paged(q[:3], p.cache, p.dev_table[:3].contiguous(), few, workspace=ws)
     assert torch.equal(got, ef.attention_paged(q[:3], p.cache, p.dev_table[:3].contiguous(), few))
+
+
+@pytest.mark.parametrize("Tk,B", [(900, 1), (5000, 1), (1000, 8)])
+def test_packed_workspace_of_the_largest_call(Tk, B):
+    """One made for the longest chunks serves shorter ones, whose keys are cut into more parts."""
+    announce(f"a packed workspace for smaller calls, {Tk} keys of {B}")
+    most = 200
+    ws = ef.make_packed_workspace(torch.empty(most, 32, 128, device="cuda"),
+                                  torch.empty(Tk, 8, 128, device="cuda"), B)
+    ws[ef.COUNTER_REGION_BYTES:] = 0xff  # (NaN, if anything were read before it was written)
+    keys = [Tk // B + (-1) ** i * 20 * (B > 1) for i in range(B)]
+    for T in (most, 128, 127, 20, 16, 15, 9, 8):
+        new = [T // B] * B
+        got = run_packed((32, 8, 128, new, keys, True), workspace=ws)
+        assert torch.equal(got, run_packed((32, 8, 128, new, keys, True))), T
+        assert not ef.workspace_counters(ws).any()

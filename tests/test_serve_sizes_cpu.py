@@ -10,7 +10,7 @@ from paper_2609_12330_amd import ef_attention as ef
 pytestmark = pytest.mark.skipif(not os.path.exists(ef.LIB_PATH), reason="libef_attention.so not built")
 
 A = 0x10000  # a fake device address, never dereferenced
-SHAPE, WS = 2, 7
+SHAPE, MISALIGNED, WS = 2, 5, 7
 
 paged_size = ef.ef_attention_paged_workspace_size
 packed_size = ef.ef_attention_packed_workspace_size
@@ -63,3 +63,41 @@ def test_paged_workspace_of_one_chunk():
     """Each step of a growing chunk, where a head's workgroups go from two to one."""
     sizes = [paged_size(8192, 16, 32, 8, 128, n) for n in range(1, 3000)]
     assert sizes == sorted(sizes) and sizes[-1] < 2 ** 27
+
+
+HEADS = [(32, 8, 128), (64, 8, 64), (12, 12, 64), (6, 3, 128), (16, 1, 128), (3000, 1000, 64)]
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", HEADS)
+def test_packed_workspace_serves_smaller_calls(Hq, Hkv, D):
+    rng = random.Random(Hq)
+    for _ in range(4000):
+        T, Tk, B = spread(rng, 50000), spread(rng, 200000), spread(rng, 3000)
+        large = packed_size(T, Tk, B, Hq, Hkv, D)
+        for smaller in ((spread(rng, T), spread(rng, Tk), spread(rng, B)), (spread(rng, T), Tk, B),
+                        (max(T - 1, 1), Tk, B), (T, max(Tk - 1, 1), B), (T, Tk, max(B - 1, 1))):
+            assert packed_size(*smaller, Hq, Hkv, D) <= large, (T, Tk, B, smaller)
+
+
+@pytest.mark.parametrize("B,Tk", [(1, 900), (1, 5000), (8, 1000)])
+def test_packed_workspace_of_one_chunk(B, Tk):
+    """Each step of growing chunks, across the border where parts become longer."""
+    sizes = [packed_size(T, Tk, B, 32, 8, 128) for T in range(1, 300)]
+    assert sizes == sorted(sizes) and sizes[0] > 0
+    assert packed_size(300, 512, B, 32, 8, 128) == 0  # (nothing is cut)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", HEADS)
+def test_packed_calls_take_the_workspace_of_larger_ones(Hq, Hkv, D):
+    """Of that size it is enough, or where the call cuts nothing not looked at. (The address is not
+    aligned, which is found behind the size; calls that cut nothing are left out.)"""
+    rng = random.Random(Hkv)
+    for _ in range(2000):
+        T, Tk, B = spread(rng, 50000), spread(rng, 200000), spread(rng, 3000)
+        t, tk, b = spread(rng, T), spread(rng, Tk), spread(rng, B)
+        if tk <= 1024:
+            continue
+        size = packed_size(T, Tk, B, Hq, Hkv, D)
+        call = (A, A, A, A, A, A, t, tk, b, Hq, Hkv, D, 0.1, 1, A + 8)
+        assert ef.ef_attention_packed(*call, size, None) == MISALIGNED, (T, Tk, B, t, tk, b)
+        assert ef.ef_attention_packed(*call, 1000, None) == WS
