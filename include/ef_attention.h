@@ -621,7 +621,7 @@ ef_status ef_cache_read(const void* k_cache, const void* v_cache, const float* k
 /*
  * Attention of new tokens over a paged cache that holds them: row (t, hq) of new token i of
  * sequence b sees the positions up to its own, len_b - n_b + i. A row that sees none is 0.
- *   q, o      : [T][Hq][D] bf16.
+ *   q, o      : [T][Hq][D] bf16; o may be q.
  *   lengths   : [B] int32, clamped to [0, width * page].
  *   starts    : [B + 1] int32, or NULL: every sequence has T / B new tokens (T % B == 0).
  *   max_queries : most new tokens of a sequence; of one that has more, only the first
@@ -651,7 +651,7 @@ size_t ef_attention_paged_workspace_size(int T, int B, int Hq, int Hkv, int D, i
  * sequence's packed keys. With causal != 0 it sees key j iff j <= i + len_b - n_b (n_b tokens,
  * len_b keys: a prompt where they are equal, a chunk behind earlier keys otherwise), else all.
  * A row that sees no key is 0.
- *   q, o     : [T][Hq][D] bf16;  k, v : [Tk][Hkv][D] bf16.
+ *   q, o     : [T][Hq][D] bf16, o may be q;  k, v : [Tk][Hkv][D] bf16.
  *   starts   : [B + 1] int32, the sequences' rows of q.
  *   k_starts : [B + 1] int32, their rows of k and v.
  *   workspace : ef_attention_packed_workspace_size(...) bytes, 16-byte aligned (may be NULL where

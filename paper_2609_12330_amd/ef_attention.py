@@ -1220,7 +1220,7 @@ def attention_paged(q, cache: PagedCache, table, lengths, starts=None,
     """Attention of the new tokens q [T, Hq, D] of B sequences over their cached keys, their own
     among them, through ef_attention_paged; token i of n sees the positions up to lengths[b] - n +
     i. starts [B + 1] int32 are the sequences' rows, T / B each without it; max_queries is the
-    most rows of a sequence, needed with starts. Returns bf16 shaped like q."""
+    most rows of a sequence, needed with starts. Returns bf16 shaped like q; `out` may be q."""
     torch = _torch()
     bf16, i32 = torch.bfloat16, torch.int32
     dev = q.get_device()
@@ -1274,7 +1274,7 @@ def attention_packed(q, k, v, starts, k_starts=None, causal: bool = True,
     """Attention of packed sequences through ef_attention_packed: rows starts[b] .. starts[b + 1] -
     1 of q [T, Hq, D] over rows k_starts[b] .. k_starts[b + 1] - 1 of k, v [Tk, Hkv, D] (starts,
     where k_starts is left out), the last ones of which are the rows' own with `causal`. Returns
-    bf16 shaped like q."""
+    bf16 shaped like q; `out` may be q."""
     torch = _torch()
     bf16, i32 = torch.bfloat16, torch.int32
     dev = q.get_device()
