@@ -576,8 +576,9 @@ size_t ef_attention_shared_prefix_workspace_size(int B, int Hq, int Hkv, int Sq,
  *   x, out    : [T][H][D] bf16; they may be the same buffer, but not overlap otherwise.
  *   positions : [T] int32, any value.
  *   turns     : [rot / 2] double, device, 16-byte aligned: turns (of 2 pi) per position. Angles
- *               are formed in 64 bits, so far positions lose nothing; amplitude cos and amplitude
- *               sin are rounded to fp32, and so is each product and sum, and the result to bf16.
+ *               are formed in 64 bits (with turns of at most 1 / 2 pi they are off by 2^-25 turns at
+ *               most); amplitude cos and amplitude sin are rounded to fp32, and so is each product
+ *               and sum, and the result to bf16.
  *   rot       : a multiple of 16, 16 .. D.
  * Errors: EF_ERR_INVALID_ROPE; others as for ef_attention_fwd.
  */
@@ -632,7 +633,9 @@ ef_status ef_cache_read(const void* k_cache, const void* v_cache, const float* k
  *               serves smaller ones.
  * Limits beside those of the other calls: B (width page / 64 + 32) < 2^31 (units of work that are
  * counted in 32 bits), and max_queries Hq / 32 <= 2^23 (workgroups of a launch).
- * The keys of all sequences are dealt evenly to the compute units, whatever their lengths.
+ * The keys of all sequences are dealt evenly to the compute units, whatever their lengths. (Not so
+ * the rows: 32 of a kv head share a walk, and the more there are, the fewer workgroups a walk has.
+ * A chunk of hundreds of tokens and single tokens of other sequences take less time in two calls.)
  * Results depend on how they are dealt, that is on the other sequences of the call, in the last
  * bits; the same call gives the same bits.
  */

@@ -14,11 +14,14 @@
 // order of their parts' keys, longest first, and the tiles of one from its last rows on, so that
 // the last workgroups to start are the shortest.
 //
-// What bounds it: the matrix core and the power limit, as for the prefill kernel: 16 prompts of 101
-// to 4096 tokens of 32/8 heads of 128 (774 GFLOP) 785 to 800 us, 0.97 to 0.99 PFLOP/s; 16 equal ones of
-// 2048 603 us, where the prefill kernel on padded tensors takes 620. Chunks of 700 and 1500
-// tokens of 64/8 heads of 64 over 9001 and 16001 keys (382 GFLOP) 410 to 430 us, 0.89 to 0.93: 1104
-// workgroups of two lengths on 512 places. Finer parts lose more than they even out: at most a half
+// What bounds it: the power limit and the issue of a step, as for the causal prefill kernel. 16 prompts
+// of 101 to 4096 tokens of 32/8 heads of 128 (774 GFLOP) 780 to 800 us, 0.97 to 0.99 PFLOP/s: the clock
+// is at 1.95 GHz, the matrix cores are busy 49% of the time and waves wait 28% of theirs (the first
+// forty calls after a pause take up to 970 us, until the clock has settled); 16 equal ones of 2048 590
+// to 603 us, where the prefill kernel on padded tensors takes 620. Chunks of 700 and 1500 tokens of
+// 64/8 heads of 64 over 9001 and 16001 keys (382 GFLOP) 400 to 432 us, 0.88 to 0.95: the softmax of a
+// score is the same beside half the products (1.93 GHz, matrix cores 45% busy), and 1104 workgroups of
+// two lengths share 512 places. Finer parts lose more than they even out: at most a half
 // / a third / a quarter of a place's share 410 -> 440 / 490 / 480 us. Three short prompts 11.4 us:
 // round trips (sequences, first tiles, rows) and five key tiles.
 #include "ef_serve.hpp"

@@ -139,10 +139,12 @@ ef_status paged_plan(PagedPlan& p, int T, int B, int Hq, int Hkv, int D, int max
 // Launch shape of attention of packed sequences: see PackedParams. Row tiles of a kv head are at
 // most G T / 128 + B, and their keys are cut into parts of at least `least` tiles: 128 rows' states
 // cost as much as ten tiles, with the second launch that joins them, those of a few rows little
-// more than that launch. At least 4 / 8 / 16 tiles: one prompt of 777 tokens of 32/8 heads of 128
-// [13 tiles] 41.9 / 41.7 / 19.2 us, one of 512 [8] 30.7 / 14.9 / 15.0; one token of 16 sequences of
-// 4 heads over 90 to 2311 keys 15.3 / 16.9 / 23.3, 19 to 44 of 9 of 16/4 heads over 2747 to 7262 39.3
-// / 40.8 / 47.0.
+// more than that launch. At least 4 / 16 tiles: one prompt of 777 tokens of 32/8 heads of 128 [13
+// tiles] 38.7 / 19.0 us; one token of 16 sequences of 4 heads over 90 to 2311 keys 16.5 / 23.3, 15 of
+// one of 32/8 heads over 5000 18.0 / 24.3. Between the border (64 rows of a sequence) and a full tile
+// either may be faster: 24 tokens of 32/8 heads over 5000 keys 19.5 / 26.7, over 32768 41.5 / 36.2, 25
+// of 4 sequences over 8000 37.9 / 33.7, 19 to 44 of 9 of 16/4 heads over 2747 to 7262 37.2 / 39.4, the
+// longer chunks over the shorter contexts 35.6 / 33.7.
 constexpr int kLeastFull = 16, kLeastFew = 4, kFewRows = 64;
 // Key tiles of a call that are not cut, whatever the rows: the second launch costs more than two parts
 // save (one token over 320 keys of 32/8 heads of 128, cut / whole 11.1 / 9.1 us, over 512 11.9 / 11.7,
