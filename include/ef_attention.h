@@ -662,6 +662,8 @@ size_t ef_attention_paged_workspace_size(int T, int B, int Hq, int Hkv, int D, i
  *              where few rows have many keys, behind the counter region of ef_attention_splitkv's
  *              workspace, which is not touched: one workspace serves both. Calls that overlap in
  *              time must not share one.
+ * Limit beside those of the other calls: T Hq / 128 + B Hkv <= 2^23 (workgroups of a launch, partial
+ * states among them).
  */
 ef_status ef_attention_packed(const void* q, const void* k, const void* v, const int* starts,
                               const int* k_starts, void* o, int T, int Tk, int B, int Hq, int Hkv,

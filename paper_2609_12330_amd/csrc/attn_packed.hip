@@ -15,7 +15,7 @@
 // the last workgroups to start are the shortest.
 //
 // What bounds it: the power limit and the issue of a step, as for the causal prefill kernel. 16 prompts
-// of 101 to 4096 tokens of 32/8 heads of 128 (774 GFLOP) 780 to 800 us, 0.97 to 0.99 PFLOP/s: the clock
+// of 101 to 4096 tokens of 32/8 heads of 128 (774 GFLOP) 770 to 800 us, 0.97 to 1.01 PFLOP/s: the clock
 // is at 1.95 GHz, the matrix cores are busy 49% of the time and waves wait 28% of theirs (the first
 // forty calls after a pause take up to 970 us, until the clock has settled); 16 equal ones of 2048 590
 // to 603 us, where the prefill kernel on padded tensors takes 620. Chunks of 700 and 1500 tokens of

@@ -34,6 +34,14 @@ def test_chunk_beside_many_sequences(Hq, H, D, page, chunk, keys, at, B, e4m3):
     run_paged((Hq, H, D, page, new, lengths), e4m3)
 
 
+@pytest.mark.parametrize("H", [1030, 2100])
+def test_many_heads(H):
+    """A workgroup to each head: counters where there are enough of them, none where not, and nothing to
+    join."""
+    announce(f"{H} kv heads")
+    run_paged((2 * H, H, 64, 16, [1, 2], [40, 7]), False)
+
+
 def test_paged_workspace_of_the_largest_call():
     """One made for a chunk of 520 tokens serves all shorter ones, with the same results as their own."""
     announce("a paged workspace for smaller calls")

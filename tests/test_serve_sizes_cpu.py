@@ -101,3 +101,12 @@ def test_packed_calls_take_the_workspace_of_larger_ones(Hq, Hkv, D):
         call = (A, A, A, A, A, A, t, tk, b, Hq, Hkv, D, 0.1, 1, A + 8)
         assert ef.ef_attention_packed(*call, size, None) == MISALIGNED, (T, Tk, B, t, tk, b)
         assert ef.ef_attention_packed(*call, 1000, None) == WS
+
+
+def test_most_packed_sequences():
+    """T Hq / 128 + B Hkv workgroups of a launch, up to 2^23 (fewer for sequences of one token)."""
+    call = (A, A, A, A, A, A)
+    assert ef.ef_attention_packed(*call, 2 ** 20, 2 ** 21, 2 ** 19, 32, 8, 128, 0.1, 1, None, 0,
+                                  None) == WS
+    for T, B in ((2 ** 22, 2 ** 22), (2 ** 25, 2 ** 19)):
+        assert ef.ef_attention_packed(*call, T, 2 ** 21, B, 32, 8, 128, 0.1, 1, None, 0, None) == SHAPE
